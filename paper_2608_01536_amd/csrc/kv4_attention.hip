@@ -271,7 +271,7 @@ __device__ __forceinline__ void attend_tile(const Keys<D>& k, const Values<D>& v
     const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);   // nothing seen yet: stays below all
     const float r = __builtin_amdgcn_exp2f(s.ref - ref);
     s.top = top, s.vmax = vm, s.ref = ref;
-    s.limit = top + kSlack / cs;
+    s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
     s.l *= r;
     s.pm *= r;
 #pragma unroll
@@ -631,7 +631,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkKeys<D>& k, const ChunkV
     const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);
     const float r = __builtin_amdgcn_exp2f(s.ref - ref);
     s.top = top, s.vmax = vm, s.ref = ref;
-    s.limit = top + kSlack / cs;
+    s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
     s.l *= r;
     s.pm *= r;
 #pragma unroll
