@@ -34,7 +34,7 @@ struct Span {
 
 __device__ __forceinline__ Span span_of(const Kv4Args& a, int seq) {
   Span s;
-  s.len = a.kv_len[seq];
+  s.len = max(a.kv_len[seq], 0);   // no positions; from here on a position's arithmetic fits in 32 bits
   if (a.q_start) {
     const int lo = min(max(a.q_start[seq], 0), a.n_tokens), hi = min(max(a.q_start[seq + 1], 0), a.n_tokens);
     s.first = lo;

@@ -27,3 +27,26 @@ def test_scores_that_vanish_under_a_window(env, which, tiny, D):  # noqa: F811
     q = (q * 2.0 ** -115 if tiny == "queries" else q).to(s.dtype)
     assert (q != 0).any(-1).all()
     _attend(env, s, heads, window=window, q=q, scale=2.0 ** -120 if tiny == "scale" else None, only=only)
+
+
+@pytest.mark.parametrize("length", [-1, -100, -(2 ** 31) + 5, -(2 ** 31)])
+@pytest.mark.parametrize("shape", [(16, 4, 2), (300, 96, 96)], ids=str)
+def test_lengths_below_zero(env, length, shape):  # noqa: F811
+    """A sequence of less than no positions: nothing is written, gathered or seen."""
+    torch, celty = env
+    n, heads, kv_heads = shape
+    s = Sequences(env, [n], [n], kv_heads, 64, 32, "float16", seed=32)
+    s.append()
+    before = s.arrays()
+    s.kv_len.fill_(length)
+    q = torch.randn(n, heads, 64, generator=s.g, device="cuda").half()
+    for seqs, t in ((s.seqs, n), (celty.Kv4Seqs(s.table, s.kv_len), 1)):
+        out = torch.full_like(q[:t], float("nan"))
+        celty.celty_kv4_attention(s.cache, seqs, q[:t], out, celty.new_kv4_workspace(s.cache, seqs, t, heads))
+        assert (out == 0).all()
+        k, v = torch.full_like(s.k[0][:t], 3.0), torch.full_like(s.v[0][:t], 3.0)
+        celty.celty_kv4_append(s.cache, seqs, k, v)
+        celty.celty_kv4_gather(s.cache, seqs, k, v)
+        assert (k == 0).all() and (v == 0).all()
+    for a, b in zip(s.arrays(), before):
+        assert (a.view("u1") == b.view("u1")).all()
