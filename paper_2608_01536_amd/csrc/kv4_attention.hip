@@ -33,7 +33,7 @@
 // only when a probability times its value scale would leave fp16's range
 // (2^15, against 2^11 when it is set), so most tiles need no exchange for the
 // maximum and no scaling of the output.  M includes the largest value scale
-// seen: what is rounded to fp16 is p s, at its best resolution whatever the
+// that the query has seen: what is rounded to fp16 is p s, at its best resolution whatever the
 // values' magnitude, and one that is 2^-25 of the largest is still kept to a
 // part in 2^11 (2^-35 to one bit).  The sums of p and of p (m + 8 s) take the
 // unrounded p, in fp32.
@@ -73,6 +73,7 @@ constexpr float kLow = -1e30f;       // a reference below every score
 constexpr float kHeadroom = 11.0f;   // log2 of p s when the reference is set
 constexpr float kLimit = 15.0f;      // and when it must be raised
 constexpr float kSlack = (kLimit - kHeadroom) / 2;
+constexpr float kScaleMargin = 1 << static_cast<int>(kSlack);
 constexpr int kMaxSplits = 128;      // of a unit: (L, M) of all fit the join's LDS
 constexpr int kMinBlocks = 16;       // least tiles of 32 positions a split takes
 
@@ -173,7 +174,7 @@ template <int D>
 struct Values {
   uint32_t c[D / 16];      // channels 64 n + 4 r + 0..3 at positions 8 g ..
   uint32_t p[8];
-  uint32_t own;            // parameters of position lane % 32, for the largest scale
+  uint32_t own;            // parameters of position lane % 32, for the largest scale of a tile seen whole
 };
 
 // Loads go through a buffer descriptor of the 32 positions: a scalar base,
@@ -230,11 +231,21 @@ struct Running {
   float top, limit;     // the largest score the reference was set from, and the score that raises it
   float vmax;           // the largest value scale it was set from
   float ref;            // the reference M
+  float scale_limit;    // the value scale of a tile seen whole that raises every query's
 };
+
+// The largest value scale of those given; NaN counts for nothing.
+template <int N>
+__device__ __forceinline__ float largest_scale(const half2_t (&p)[N]) {
+  half2_t m = p[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = __builtin_elementwise_max(m, p[i]);
+  return static_cast<float>(m[0]);
+}
 
 template <int D>
 __device__ __forceinline__ void attend_tile(const Keys<D>& k, const Values<D>& v, const half8_t (&q)[D / 32], float cs, float qm, bool masked,
-                                            int from, int to, int seen_to, const Bits& bits, Running<D>& s) {
+                                            int from, int to, const Bits& bits, Running<D>& s) {
   __builtin_amdgcn_sched_barrier(0);
   float4_t acc[2] = {};
 #pragma unroll
@@ -251,7 +262,7 @@ __device__ __forceinline__ void attend_tile(const Keys<D>& k, const Values<D>& v
     x[i] = fmaf(scale_of(k.p[i]), acc[i / 4][i % 4], fmaf(minimum_of(k.p[i]), qm, 0.0f));
     vp[i] = __builtin_bit_cast(half2_t, v.p[i]);
   }
-  float sm = scale_of(v.own);
+  float sm = scale_of(v.own), scale_limit = s.scale_limit;
   if (masked) {   // the same for the whole wavefront
     // neither what a hidden position's score is nor its value's parameters may matter
 #pragma unroll
@@ -260,22 +271,28 @@ __device__ __forceinline__ void attend_tile(const Keys<D>& k, const Values<D>& v
       x[i] = hidden ? -INFINITY : x[i];
       vp[i] = hidden ? half2_t{} : vp[i];
     }
-    sm = (threadIdx.x & 31) <= seen_to ? sm : 0.0f;
+    sm = largest_scale(vp);
+    scale_limit = s.vmax * kScaleMargin;
   }
   const float xm = largest(x);
   // p s <= 2^limit holds while the score's and the scale's excess over what the
-  // reference was set from are within half the margin each
-  if (__any(xm > s.limit || sm > s.vmax * (1 << static_cast<int>(kSlack)))) {
-    const float top = column_max(fmaxf(s.top, xm));
-    const float vm = row_max(column_max(fmaxf(s.vmax, sm)));
-    const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);   // nothing seen yet: stays below all
-    const float r = __builtin_amdgcn_exp2f(s.ref - ref);
-    s.top = top, s.vmax = vm, s.ref = ref;
-    s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
-    s.l *= r;
-    s.pm *= r;
+  // reference was set from are within half the margin each.  A tile that all
+  // queries see whole raises all of them for its scales, another each query for
+  // those it sees: no result depends on what another query's window holds.
+  if (__any(xm > s.limit || sm > scale_limit)) {
+    const float xc = column_max(xm), sc = masked ? column_max(sm) : row_max(column_max(sm));
+    if (xc > s.limit || sc > scale_limit) {   // this query's own
+      const float top = fmaxf(s.top, xc), vm = fmaxf(s.vmax, sc);
+      const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);   // nothing seen yet: stays below all
+      const float r = __builtin_amdgcn_exp2f(s.ref - ref);
+      s.top = top, s.vmax = vm, s.ref = ref;
+      s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
+      s.l *= r;
+      s.pm *= r;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) s.o[c] *= r;
+      for (int c = 0; c < D / 16; ++c) s.o[c] *= r;
+    }
+    if (!masked && sc > scale_limit) s.scale_limit = sc * kScaleMargin;
   }
   half8_t b;   // probabilities times the values' scales
 #pragma unroll
@@ -396,7 +413,7 @@ __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args 
   load_query<T, D, D / 4>(static_cast<const T*>(f.q) + (sp.first + qi) * f.q_token + qh * f.q_head + g * (D / 4), f.scale, q, cs, qm);
   const Bits bits = number_bits();
   Running<D> s = {};
-  s.top = kLow, s.limit = kLow, s.ref = kLow, s.vmax = 0x1p-30f;
+  s.top = kLow, s.limit = kLow, s.ref = kLow, s.vmax = s.scale_limit = 0x1p-30f;
   const int k_lane = (8 * (r >> 2) + (r & 3)) * (D / 2) + g * (D / 8), v_lane = (g * D + 4 * r) * 4, p_lane = 32 * g;
   const int32_t* table = a.table + static_cast<int64_t>(seq) * a.table_stride;
   const int shift = a.page_log2 - 5;   // tiles of a page, log2
@@ -424,7 +441,7 @@ __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args 
       // this lane's positions t0 + 8 g + from .. to; most tiles are seen whole
       const bool whole = page0 >= 0 && t0 + 31 <= pos_lo && t0 >= whole_from;
       const int from = lane_from - t0 - 8 * g, to = page0 < 0 ? -1 : lane_to - t0 - 8 * g;
-      attend_tile<D>(keys[now], values, q, cs, qm, !whole, from, to, page0 < 0 ? -1 : pos_hi - t0, bits, s);
+      attend_tile<D>(keys[now], values, q, cs, qm, !whole, from, to, bits, s);
       page0 = page1;
       page1 = page2;
       b += NW;
@@ -554,7 +571,7 @@ template <int D>
 struct ChunkValues {
   uint32_t c[2][D / 32];   // octets h and 2 + h, channels (D / 32) r ..
   uint32_t p[16];
-  uint32_t own;            // parameters of position lane % 32
+  uint32_t own;            // parameters of position lane % 32, for the largest scale of a tile seen whole
 };
 
 __device__ __forceinline__ void load_params16(const __amdgpu_buffer_rsrc_t rs, int p_lane, uint32_t (&out)[16]) {
@@ -597,12 +614,12 @@ __device__ __forceinline__ void load_chunk_values(const Kv4Args& a, int64_t slot
 template <int D>
 struct ChunkRunning {
   float16_t o[D / 32];   // channel (D / 32) row + tile
-  float l, pm, top, limit, vmax, ref;
+  float l, pm, top, limit, vmax, ref, scale_limit;
 };
 
 template <int D>
 __device__ __forceinline__ void attend_chunk(const ChunkKeys<D>& k, const ChunkValues<D>& v, const half8_t (&q)[D / 16], float cs,
-                                             float qm, bool masked, int from, int to, int seen_to, const Bits& bits, ChunkRunning<D>& s) {
+                                             float qm, bool masked, int from, int to, const Bits& bits, ChunkRunning<D>& s) {
   float16_t acc = {};
 #pragma unroll
   for (int j = 0; j < D / 16; ++j) acc = mfma32(operand_of(k.c[j]), q[j], acc);
@@ -613,7 +630,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkKeys<D>& k, const ChunkV
     x[i] = fmaf(scale_of(k.p[i]), acc[i], fmaf(minimum_of(k.p[i]), qm, 0.0f));
     vp[i] = __builtin_bit_cast(half2_t, v.p[i]);
   }
-  float sm = scale_of(v.own);
+  float sm = scale_of(v.own), scale_limit = s.scale_limit;
   if (masked) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -622,20 +639,24 @@ __device__ __forceinline__ void attend_chunk(const ChunkKeys<D>& k, const ChunkV
       x[i] = hidden ? -INFINITY : x[i];
       vp[i] = hidden ? half2_t{} : vp[i];
     }
-    sm = (threadIdx.x & 31) <= seen_to ? sm : 0.0f;
+    sm = largest_scale(vp);
+    scale_limit = s.vmax * kScaleMargin;
   }
   const float xm = largest(x);
-  if (__any(xm > s.limit || sm > s.vmax * (1 << static_cast<int>(kSlack)))) {
-    const float top = halves_max(fmaxf(s.top, xm));
-    const float vm = row_max(column_max(fmaxf(s.vmax, sm)));   // over the 32 positions, the same for all columns
-    const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);
-    const float r = __builtin_amdgcn_exp2f(s.ref - ref);
-    s.top = top, s.vmax = vm, s.ref = ref;
-    s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
-    s.l *= r;
-    s.pm *= r;
+  if (__any(xm > s.limit || sm > scale_limit)) {
+    const float xc = halves_max(xm), sc = masked ? halves_max(sm) : row_max(column_max(sm));   // unmasked: over the 32 positions
+    if (xc > s.limit || sc > scale_limit) {
+      const float top = fmaxf(s.top, xc), vm = fmaxf(s.vmax, sc);
+      const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);
+      const float r = __builtin_amdgcn_exp2f(s.ref - ref);
+      s.top = top, s.vmax = vm, s.ref = ref;
+      s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
+      s.l *= r;
+      s.pm *= r;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) s.o[c] *= r;
+      for (int c = 0; c < D / 32; ++c) s.o[c] *= r;
+    }
+    if (!masked && sc > scale_limit) s.scale_limit = sc * kScaleMargin;
   }
   half8_t b[2];
 #pragma unroll
@@ -685,7 +706,7 @@ __global__ __launch_bounds__(kChunkWaves* kWave, 2) void chunk_kernel(Kv4Args a,
   const int lane_to = max(p0 + qi, -1), lane_from = earliest(lane_to), whole_from = earliest(pos_hi);
   const Bits bits = number_bits();
   ChunkRunning<D> s = {};
-  s.top = kLow, s.limit = kLow, s.ref = kLow, s.vmax = 0x1p-30f;
+  s.top = kLow, s.limit = kLow, s.ref = kLow, s.vmax = s.scale_limit = 0x1p-30f;
   // tiles this wavefront's columns see
   int b = max(first, earliest(pos_lo) >> 5);
   const int end = cols > 0 && pos_hi >= 0 ? min(last, (pos_hi >> 5) + 1) : 0;
@@ -716,7 +737,7 @@ __global__ __launch_bounds__(kChunkWaves* kWave, 2) void chunk_kernel(Kv4Args a,
       const int t0 = b << 5;
       const bool whole = page0 >= 0 && t0 + 31 <= pos_lo && t0 >= whole_from;
       const int from = lane_from - t0 - 8 * h, to = page0 < 0 ? -1 : lane_to - t0 - 8 * h;
-      attend_chunk<D>(keys[now], values, q, cs, qm, !whole, from, to, page0 < 0 ? -1 : pos_hi - t0, bits, s);
+      attend_chunk<D>(keys[now], values, q, cs, qm, !whole, from, to, bits, s);
       page0 = page1;
       page1 = page2;
       ++b;

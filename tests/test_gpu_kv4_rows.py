@@ -50,3 +50,54 @@ def test_lengths_below_zero(env, length, shape):  # noqa: F811
         assert (k == 0).all() and (v == 0).all()
     for a, b in zip(s.arrays(), before):
         assert (a.view("u1") == b.view("u1")).all()
+
+
+def _set_params(torch, s, first, last, scale, minimum):
+    """Key and value parameters of positions first..last-1 of the one sequence."""
+    t = torch.arange(first, last, device="cuda")
+    pages, slots = s.table[0].long()[t // s.page], t % s.page
+    p = torch.tensor([scale, minimum], device="cuda").half()
+    for x in (s.cache.k_params, s.cache.v_params):
+        x[pages, :, slots] = p
+
+
+@pytest.mark.parametrize("which", list(WINDOWED))
+@pytest.mark.parametrize("scale", [float("inf"), 65504.0, float("nan"), float("-inf")])
+@pytest.mark.parametrize("D", [64, 128])
+def test_positions_before_every_window_do_not_matter(env, which, scale, D):  # noqa: F811
+    """A caller that keeps the last `window` tokens only: whatever is in the
+    memory of the others, the results are the same bits."""
+    torch, celty = env
+    n, m, heads, kv_heads, window, only = WINDOWED[which]
+    s = Sequences(env, [n], [m], kv_heads, D, 32, "float16", seed=33, ranges=(1.0, 2.0 ** -8))
+    s.fill()
+    q, out, ws = _attend(env, s, heads, window=window, only=only)
+    first = n - m - window + 1
+    assert first > 0
+    _set_params(torch, s, 0, first, scale, 1.0)
+    got = torch.full_like(out, float("nan"))
+    celty.celty_kv4_attention(s.cache, s.seqs, q, got, ws, window=window)
+    assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("which", list(WINDOWED))
+@pytest.mark.parametrize("window", [True, False])
+def test_later_tokens_do_not_matter(env, which, window):  # noqa: F811
+    """A token's result is the same bits whatever the tokens after it hold,
+    values far above its own among them."""
+    torch, celty = env
+    n, m, heads, kv_heads, w, only = WINDOWED[which]
+    w = w if window else 0
+    s = Sequences(env, [n], [m], kv_heads, 64, 32, "float16", seed=34, ranges=(1.0, 2.0 ** -8))
+    s.fill()
+    q, out, ws = _attend(env, s, heads, window=w, only=only)
+    for keep in (1, m // 2, m - 1):   # tokens of the call
+        a = n - m + keep
+        s.v[0][a:] = 20000.0 * torch.randn(n - a, kv_heads, 64, generator=s.g, device="cuda").clamp(-3, 3).half()
+        s.k[0][a:] *= 8.0
+        s.append()
+        got = torch.full_like(out, float("nan"))
+        celty.celty_kv4_attention(s.cache, s.seqs, q, got, ws, window=w)
+        assert torch.equal(got[:keep], out[:keep]), keep
+        s = Sequences(env, [n], [m], kv_heads, 64, 32, "float16", seed=34, ranges=(1.0, 2.0 ** -8))
+        s.fill()
