@@ -33,10 +33,12 @@
 // only when a probability times its value scale would leave fp16's range
 // (2^15, against 2^11 when it is set), so most tiles need no exchange for the
 // maximum and no scaling of the output.  M includes the largest value scale
-// that the query has seen: what is rounded to fp16 is p s, at its best resolution whatever the
-// values' magnitude, and one that is 2^-25 of the largest is still kept to a
-// part in 2^11 (2^-35 to one bit).  The sums of p and of p (m + 8 s) take the
-// unrounded p, in fp32.
+// that the query has seen: what is rounded to fp16 is p s, at its best
+// resolution whatever the values' magnitude, and one that is 2^-25 of the largest
+// is still kept to a part in 2^11 (2^-35 to one bit).  The sums of p and of
+// p (m + 8 s) take the unrounded p, in fp32.  M is kept in two parts, the largest
+// score and the rest: scores are taken as differences from the former (the
+// addend of a product that is made anyway), so that their size does not matter.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -69,7 +71,7 @@ struct AttnArgs {
   float* partial;         // per unit and split: 16 x D sums, then 16 x (L, M)
 };
 
-constexpr float kLow = -1e30f;       // a reference below every score
+constexpr float kLow = -3e38f;       // a reference below every score
 constexpr float kHeadroom = 11.0f;   // log2 of p s when the reference is set
 constexpr float kLimit = 15.0f;      // and when it must be raised
 constexpr float kSlack = (kLimit - kHeadroom) / 2;
@@ -228,11 +230,38 @@ template <int D>
 struct Running {
   float4_t o[D / 16];   // channels 64 (t / 4) + 16 g + 4 i + t % 4
   float l, pm;          // this lane's part of sum p and sum p m
-  float top, limit;     // the largest score the reference was set from, and the score that raises it
-  float vmax;           // the largest value scale it was set from
-  float ref;            // the reference M
+  float top;            // the largest score the reference was set from; scores are taken from it on
+  float limit;          // the score above it that raises it, kLow until something is seen
+  float vmax;           // the largest value scale the reference was set from
+  float shift;          // cs top less the reference M
   float scale_limit;    // the value scale of a tile seen whole that raises every query's
 };
+
+// Sets a query's reference from scores up to xc above its present one and value
+// scales up to sc, takes the scores x from it on and returns the factor of the
+// sums so far, of which those of p are brought along.  Scores are compared as
+// differences from the largest: however large they are, its exponent is exact.
+template <int N, typename S>
+__device__ __forceinline__ float raise_reference(float xc, float sc, float cs, S& s, float (&x)[N]) {
+  const bool before = s.limit > kLow, seen = before || xc > kLow;   // nothing seen: all sums are zero, or NaN
+  const float rise = before ? fmaxf(xc, 0.0f) : seen ? xc : 0.0f;
+  s.vmax = fmaxf(s.vmax, sc);
+  const float shift = kHeadroom - __builtin_amdgcn_logf(s.vmax);   // to base 2; what it rounds to is kept in s.shift
+  const float r = before ? __builtin_amdgcn_exp2f(fmaf(-cs, rise, shift - s.shift)) : 1.0f;
+  s.top += rise, s.shift = shift;
+  s.limit = seen ? kSlack * __builtin_amdgcn_rcpf(cs) : kLow;
+  s.l *= r;
+  s.pm *= r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] -= rise;
+  return r;
+}
+// Sums that were taken apart are joined as multiples of exp2 of their largest
+// score: the shift, which a large score would swallow, is taken off them first.
+template <typename S>
+__device__ __forceinline__ float top_score(float cs, const S& s) {
+  return s.limit > kLow ? cs * s.top : kLow;
+}
 
 // The largest value scale of those given; NaN counts for nothing.
 template <int N>
@@ -255,11 +284,11 @@ __device__ __forceinline__ void attend_tile(const Keys<D>& k, const Values<D>& v
     __builtin_amdgcn_sched_barrier(0);
   }
   __builtin_amdgcn_sched_barrier(0);   // the phases one after another: hoisted operands would cost registers
-  float x[8];   // positions 8 g + i, in units of 1 / cs
+  float x[8];   // positions 8 g + i, above the reference's score, in units of 1 / cs
   half2_t vp[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    x[i] = fmaf(scale_of(k.p[i]), acc[i / 4][i % 4], fmaf(minimum_of(k.p[i]), qm, 0.0f));
+    x[i] = fmaf(scale_of(k.p[i]), acc[i / 4][i % 4], fmaf(minimum_of(k.p[i]), qm, -s.top));
     vp[i] = __builtin_bit_cast(half2_t, v.p[i]);
   }
   float sm = scale_of(v.own), scale_limit = s.scale_limit;
@@ -282,13 +311,7 @@ __device__ __forceinline__ void attend_tile(const Keys<D>& k, const Values<D>& v
   if (__any(xm > s.limit || sm > scale_limit)) {
     const float xc = column_max(xm), sc = masked ? column_max(sm) : row_max(column_max(sm));
     if (xc > s.limit || sc > scale_limit) {   // this query's own
-      const float top = fmaxf(s.top, xc), vm = fmaxf(s.vmax, sc);
-      const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);   // nothing seen yet: stays below all
-      const float r = __builtin_amdgcn_exp2f(s.ref - ref);
-      s.top = top, s.vmax = vm, s.ref = ref;
-      s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
-      s.l *= r;
-      s.pm *= r;
+      const float r = raise_reference(xc, sc, cs, s, x);
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) s.o[c] *= r;
     }
@@ -297,7 +320,7 @@ __device__ __forceinline__ void attend_tile(const Keys<D>& k, const Values<D>& v
   half8_t b;   // probabilities times the values' scales
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float e = __builtin_amdgcn_exp2f(fmaf(cs, x[i], -s.ref)), scale = static_cast<float>(vp[i][0]);
+    const float e = __builtin_amdgcn_exp2f(fmaf(cs, x[i], s.shift)), scale = static_cast<float>(vp[i][0]);
     s.l += e;
     s.pm = fmaf(e, fmaf(scale, 8.0f, static_cast<float>(vp[i][1])), s.pm);
     b[2 * (i % 4) + i / 4] = static_cast<half_t>(fmaf(e, scale, 0.0f));   // one instruction, product and rounding
@@ -346,8 +369,10 @@ __device__ __forceinline__ void load_query(const T* q, float scale, half8_t (&ou
       out[j][2 * (n % 4) + n / 4] = static_cast<half_t>((n & 1) ? x * 0.0625f : x);
     }
   }
-  // above 0, for hidden scores are -infinity; below 2^-100 every score is as good as zero
-  cs = scale == 0.0f || big == 0.0f ? 1.0f : fmaxf(fabsf(scale) * ldexpf(1.0f, 24 + e), 0x1p-100f);
+  // above 0, for hidden scores are -infinity: scores are below 2^16 (with codes
+  // below 16, scales and minima in fp16), so under 2^-100 every one is as good as
+  // zero, and over 2^100 no two that differ share the weight
+  cs = scale == 0.0f || big == 0.0f ? 1.0f : fminf(fmaxf(ldexpf(fabsf(scale), 24 + e), 0x1p-100f), 0x1p100f);
   qm = ldexpf(kQuarter ? column_sum(sum) : halves_sum(sum), -24);
 }
 
@@ -374,7 +399,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args a, AttnArgs f) {
   constexpr int NW = kDecodeWaves, ROW = D + 4;   // padded against bank conflicts
   __shared__ float lds_o[NW][16][ROW];
-  __shared__ float lds_l[NW][16], lds_m[NW][16], lds_pm[NW][16];
+  __shared__ float lds_l[NW][16], lds_m[NW][16], lds_shift[NW][16], lds_pm[NW][16];
   __shared__ uint32_t lds_ticket;
   static_assert(sizeof(lds_o) >= 32 * kMaxSplits * sizeof(float), "(L, M) of every split");
   const int lane = threadIdx.x & (kWave - 1), r = lane & 15, g = lane >> 4;
@@ -413,7 +438,7 @@ __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args 
   load_query<T, D, D / 4>(static_cast<const T*>(f.q) + (sp.first + qi) * f.q_token + qh * f.q_head + g * (D / 4), f.scale, q, cs, qm);
   const Bits bits = number_bits();
   Running<D> s = {};
-  s.top = kLow, s.limit = kLow, s.ref = kLow, s.vmax = s.scale_limit = 0x1p-30f;
+  s.limit = kLow, s.vmax = s.scale_limit = 0x1p-30f;
   const int k_lane = (8 * (r >> 2) + (r & 3)) * (D / 2) + g * (D / 8), v_lane = (g * D + 4 * r) * 4, p_lane = 32 * g;
   const int32_t* table = a.table + static_cast<int64_t>(seq) * a.table_stride;
   const int shift = a.page_log2 - 5;   // tiles of a page, log2
@@ -454,10 +479,10 @@ __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args 
     }
   }
 
-  // join the wavefronts: common reference, then sums in their order
+  // join the wavefronts: the largest score, then sums in their order
   s.l = column_sum(s.l);
   s.pm = column_sum(s.pm);
-  if (g == 0) lds_l[wave][r] = s.l, lds_m[wave][r] = s.ref, lds_pm[wave][r] = s.pm;
+  if (g == 0) lds_l[wave][r] = s.l, lds_m[wave][r] = top_score(cs, s), lds_shift[wave][r] = s.shift, lds_pm[wave][r] = s.pm;
 #pragma unroll
   for (int c = 0; c < D / 64; ++c)
 #pragma unroll
@@ -474,7 +499,7 @@ __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args 
     for (int w = 0; w < NW; ++w) m = fmaxf(m, lds_m[w][oc]);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float e = __builtin_amdgcn_exp2f(lds_m[w][oc] - m);
+      const float e = __builtin_amdgcn_exp2f(lds_m[w][oc] - m - lds_shift[w][oc]);
       l += e * lds_l[w][oc];
       o += e * (*reinterpret_cast<const float4_t*>(&lds_o[w][oc][od]) + lds_pm[w][oc]);
     }
@@ -614,7 +639,7 @@ __device__ __forceinline__ void load_chunk_values(const Kv4Args& a, int64_t slot
 template <int D>
 struct ChunkRunning {
   float16_t o[D / 32];   // channel (D / 32) row + tile
-  float l, pm, top, limit, vmax, ref, scale_limit;
+  float l, pm, top, limit, vmax, shift, scale_limit;
 };
 
 template <int D>
@@ -627,7 +652,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkKeys<D>& k, const ChunkV
   half2_t vp[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    x[i] = fmaf(scale_of(k.p[i]), acc[i], fmaf(minimum_of(k.p[i]), qm, 0.0f));
+    x[i] = fmaf(scale_of(k.p[i]), acc[i], fmaf(minimum_of(k.p[i]), qm, -s.top));
     vp[i] = __builtin_bit_cast(half2_t, v.p[i]);
   }
   float sm = scale_of(v.own), scale_limit = s.scale_limit;
@@ -646,13 +671,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkKeys<D>& k, const ChunkV
   if (__any(xm > s.limit || sm > scale_limit)) {
     const float xc = halves_max(xm), sc = masked ? halves_max(sm) : row_max(column_max(sm));   // unmasked: over the 32 positions
     if (xc > s.limit || sc > scale_limit) {
-      const float top = fmaxf(s.top, xc), vm = fmaxf(s.vmax, sc);
-      const float ref = top == kLow ? kLow : fmaf(cs, top, log2f(vm) - kHeadroom);
-      const float r = __builtin_amdgcn_exp2f(s.ref - ref);
-      s.top = top, s.vmax = vm, s.ref = ref;
-      s.limit = top == kLow ? kLow : top + kSlack / cs;   // whatever a column sees first raises its reference
-      s.l *= r;
-      s.pm *= r;
+      const float r = raise_reference(xc, sc, cs, s, x);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) s.o[c] *= r;
     }
@@ -661,7 +680,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkKeys<D>& k, const ChunkV
   half8_t b[2];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const float e = __builtin_amdgcn_exp2f(fmaf(cs, x[i], -s.ref)), scale = static_cast<float>(vp[i][0]);
+    const float e = __builtin_amdgcn_exp2f(fmaf(cs, x[i], s.shift)), scale = static_cast<float>(vp[i][0]);
     s.l += e;
     s.pm = fmaf(e, fmaf(scale, 8.0f, static_cast<float>(vp[i][1])), s.pm);
     b[i / 8][2 * (i % 4) + (i % 8) / 4] = static_cast<half_t>(fmaf(e, scale, 0.0f));
@@ -706,13 +725,14 @@ __global__ __launch_bounds__(kChunkWaves* kWave, 2) void chunk_kernel(Kv4Args a,
   const int lane_to = max(p0 + qi, -1), lane_from = earliest(lane_to), whole_from = earliest(pos_hi);
   const Bits bits = number_bits();
   ChunkRunning<D> s = {};
-  s.top = kLow, s.limit = kLow, s.ref = kLow, s.vmax = s.scale_limit = 0x1p-30f;
+  float cs = 1.0f;
+  s.limit = kLow, s.vmax = s.scale_limit = 0x1p-30f;
   // tiles this wavefront's columns see
   int b = max(first, earliest(pos_lo) >> 5);
   const int end = cols > 0 && pos_hi >= 0 ? min(last, (pos_hi >> 5) + 1) : 0;
   if (b < end) {
     half8_t q[D / 16];
-    float cs, qm;
+    float qm;
     load_query<T, D, D / 2>(static_cast<const T*>(f.q) + (sp.first + qi) * f.q_token + qh * f.q_head + h * (D / 2), f.scale, q, cs,
                             qm);
     const int token = 8 * (2 * (r >> 4) + ((r >> 2) & 1)) + 4 * ((r >> 3) & 1) + (r & 3);
@@ -770,15 +790,16 @@ __global__ __launch_bounds__(kChunkWaves* kWave, 2) void chunk_kernel(Kv4Args a,
   }
   float* mine = f.partial + (static_cast<int64_t>(unit) * f.n_splits + split) * kChunkPart<D>;
   if (r < cols) {
+    const float unshift = __builtin_amdgcn_exp2f(-s.shift);
     // pairs of channels of the wavefront's 32 columns next to each other, so that
     // a store covers whole lines
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int e = 0; e < 4 * NT; e += 2)
-        store_through(mine + 32 * D * wave + 32 * (NT * (8 * n + 4 * h) + e) + 2 * r, s.o[e % NT][4 * n + e / NT] + s.pm,
-                      s.o[(e + 1) % NT][4 * n + (e + 1) / NT] + s.pm);
-    if (h == 0) store_through(mine + kChunkCols * D + 2 * (32 * wave + r), s.l, s.ref);
+        store_through(mine + 32 * D * wave + 32 * (NT * (8 * n + 4 * h) + e) + 2 * r,
+                      (s.o[e % NT][4 * n + e / NT] + s.pm) * unshift, (s.o[(e + 1) % NT][4 * n + (e + 1) / NT] + s.pm) * unshift);
+    if (h == 0) store_through(mine + kChunkCols * D + 2 * (32 * wave + r), s.l * unshift, top_score(cs, s));
   }
   wait_for_stores();
   __syncthreads();

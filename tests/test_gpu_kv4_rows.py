@@ -1,6 +1,7 @@
 """Attention over the 4-bit cache where queries of one tile see different
 positions: each row's result is its own.  The cache, the definition in 64 bits
 and its derived tolerance are those of tests/test_gpu_kv4.py."""
+import numpy as np
 import pytest
 
 from tests.test_gpu_kv4 import Sequences, _attend, env  # noqa: F401  (env: the fixture)
@@ -101,3 +102,49 @@ def test_later_tokens_do_not_matter(env, which, window):  # noqa: F811
         assert torch.equal(got[:keep], out[:keep]), keep
         s = Sequences(env, [n], [m], kv_heads, 64, 32, "float16", seed=34, ranges=(1.0, 2.0 ** -8))
         s.fill()
+
+
+LARGE = {"products": (1.0, 2.0 ** 13, None), "scale": (1.0, 1.0, 1e30), "largest_scale": (1.0, 1.0, 3.4e38),
+         "negative_scale": (1.0, 1.0, -1e12), "queries": (2.0 ** 118, 1.0, None), "queries_small_scale": (2.0 ** 124, 1.0, 2.0 ** -90)}
+
+
+@pytest.mark.parametrize("case", list(LARGE))
+@pytest.mark.parametrize("which", ["one", "split"] + list(WINDOWED))
+def test_scores_far_apart(env, case, which):  # noqa: F811
+    """Scores in the millions and far beyond: all of the weight is with the largest,
+    however little of it a step of fp32 there leaves to an exponential.  Rows whose
+    two largest are nearer than what the scores' sums may err by are left out:
+    (D + 8) 2^-24 of the largest sum of magnitudes, twice."""
+    torch, celty = env
+    q_range, k_range, scale = LARGE[case]
+    D = 64
+    n, m, heads, kv_heads, window, only = dict(one=(300, 1, 2, 1, 0, None), split=(9000, 1, 2, 1, 0, None), **WINDOWED)[which]
+    if case == "products":
+        q_range = 2.0 ** 13
+    s = Sequences(env, [n], [m], kv_heads, D, 32, "bfloat16", seed=35, ranges=(k_range, 1.0))
+    s.fill()
+    q = (torch.randn(m, heads, D, generator=s.g, device="cuda") * q_range).to(s.dtype)
+    assert q.isfinite().all()
+    out = torch.full_like(q, float("nan"))
+    celty.celty_kv4_attention(s.cache, s.seqs, q, out, celty.new_kv4_workspace(s.cache, s.seqs, m, heads), scale=scale, window=window)
+    assert out.isfinite().all()
+    k, v = s.values(0)
+    sign = -1.0 if scale is not None and scale < 0 else 1.0
+    factor = abs(scale) if scale is not None else D ** -0.5
+    checked = 0
+    for i in only if only is not None else range(m):
+        last = n - m + i
+        first = max(0, last - window + 1) if window else 0
+        for h in range(0, heads, 5):
+            g = h * kv_heads // heads
+            x = q[i, h].double().cpu().numpy()
+            z = sign * (k[first:last + 1, g] @ x)
+            order = np.argsort(z)
+            room = 2 * (D + 8) * 2.0 ** -24 * 2 * np.abs(x).sum() * np.abs(k[first:last + 1, g]).max()
+            if len(z) > 1 and (z[order[-1]] - z[order[-2]] <= room or (z[order[-1]] - z[order[-2]] - room) * factor < 30):
+                continue
+            checked += 1
+            want = v[first + order[-1], g]
+            # a probability of one: its rounding with the value's scale, and the output's
+            assert (np.abs(out[i, h].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -9 * np.abs(want).max()).all(), (i, h)
+    assert checked > 0
