@@ -154,7 +154,8 @@ celty_status celty_kv4_gather(const celty_kv4_cache* cache, const celty_kv4_seqs
  *
  * over the positions j of the sequence's storage with j <= p_i and, when
  * window > 0, j > p_i - window (p_i the token's position).  A token that sees
- * no position gets zeros.  Query head h reads key head h / (heads / kv_heads).
+ * no position gets zeros; one that sees any gets NaN for a query that is not
+ * finite or for a NaN key or value among them.  Query head h reads key head h / (heads / kv_heads).
  *   dtype      CELTY_F16 or CELTY_BF16: q and out, [n_tokens][heads][D].
  *   heads      a multiple of kv_heads.
  *   scale      finite.

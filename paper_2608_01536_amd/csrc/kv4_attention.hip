@@ -374,6 +374,7 @@ __device__ __forceinline__ void load_query(const T* q, float scale, half8_t (&ou
   // zero, and over 2^100 no two that differ share the weight
   cs = scale == 0.0f || big == 0.0f ? 1.0f : fminf(fmaxf(ldexpf(fabsf(scale), 24 + e), 0x1p-100f), 0x1p100f);
   qm = ldexpf(kQuarter ? column_sum(sum) : halves_sum(sum), -24);
+  if (big == INFINITY) qm = NAN;   // every score: those of -infinity alone would look like nothing seen
 }
 
 // A split's sums go past the L2 caches, which the chip's dies do not share, as

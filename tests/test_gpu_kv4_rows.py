@@ -148,3 +148,26 @@ def test_scores_far_apart(env, case, which):  # noqa: F811
             # a probability of one: its rounding with the value's scale, and the output's
             assert (np.abs(out[i, h].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -9 * np.abs(want).max()).all(), (i, h)
     assert checked > 0
+
+
+@pytest.mark.parametrize("which", ["one"] + list(WINDOWED))
+@pytest.mark.parametrize("bad", [float("-inf"), float("inf"), float("nan")])
+@pytest.mark.parametrize("positive", [True, False])
+def test_queries_that_are_not_finite(env, which, bad, positive):  # noqa: F811
+    """No softmax is left of scores of infinity: NaN, whatever their sign, and in
+    the query's own row alone."""
+    torch, celty = env
+    n, m, heads, kv_heads, window, only = dict(one=(300, 1, 2, 1, 0, None), **WINDOWED)[which]
+    s = Sequences(env, [n], [m], kv_heads, 64, 32, "float16", seed=36)
+    if positive:   # every minimum and every code of channel 5 above zero
+        s.k[0] = s.k[0].abs() + 1.0
+        s.k[0][:, :, 5] += 9.0
+    s.fill()
+    q, out, ws = _attend(env, s, heads, window=window, only=only)
+    row, h = m - 1, heads - 1
+    q[row, h, 5] = bad
+    got = torch.zeros_like(out)
+    celty.celty_kv4_attention(s.cache, s.seqs, q, got, ws, window=window)
+    assert got[row, h].isnan().all()
+    got[row, h] = out[row, h]
+    assert torch.equal(got, out)
