@@ -169,7 +169,7 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, const RowWork& w, int
   const int k = a.top_k ? a.top_k[row] : 0;
   r.k = k >= 1 && k < a.V ? k : 0;
   r.p = a.top_p ? a.top_p[row] : 1.0f;
-  if (!(r.p < 1.0f)) r.p = 1.0f;
+  r.p = r.p < 1.0f ? fmaxf(r.p, 0.0f) : 1.0f;   // a share below zero keeps the first token, as zero does
   const float m = a.min_p ? a.min_p[row] : 0.0f;
   r.min_p = m > 0.0f ? fminf(m, 1.0f) : 0.0f;   // fminf alone would make 1 of NaN
   return r;
