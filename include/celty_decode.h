@@ -213,7 +213,7 @@ typedef struct celty_filters {
  *   tokens  device int32[rows]; -1 for a row with no number to choose.
  * Weights are summed as multiples of 2^-38 of the largest, in 64-bit integers:
  * the result does not depend on timing.
- *   workspace  device, at least celty_sample_workspace_bytes(rows, V) bytes (60
+ *   workspace  device, at least celty_sample_workspace_bytes(rows, V) bytes (45
  *           KB a row, for 1024 rows at most), any contents; calls that may
  *           overlap need workspaces of their own.
  * Errors: EINVAL (null pointers, rows < 0, V < 1 or V > 2^24, bad dtype, short

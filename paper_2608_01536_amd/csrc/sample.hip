@@ -8,17 +8,22 @@
 //
 //   top     the largest (logit, lowest index) of each slice; clears the row's
 //           words for the other two;
-//   bins    counts and weights of the row by bins of the logit, 16 to a factor
-//           of two, as integers: weights are multiples of 2^-38 of the largest,
-//           so sums are exact in 64 bits and do not depend on their order;
+//   bins    counts and weights of the row by bins of the distance from the
+//           largest logit, 64 to a factor of two, as integers: weights are
+//           multiples of 2^-38 of the largest, so sums are exact in 64 bits and do
+//           not depend on their order;
 //   finish  every slice finds the bins that the cuts fall into from the row's
 //           sums; tokens above them race at once, those within are listed, and
 //           the slice that arrives last orders the list (some dozens of
 //           tokens), cuts it exactly and lets the rest race.
 //
-// A row whose cut bins hold more than the list does, or more equal logits than
-// it can order (long runs of ties, or top-k of thousands together with top-p),
-// is cut by the last slice alone, with bins of the logits' bits over the row.
+// A row whose cut bins hold more tokens than the list does (4096), or more than
+// 1024 in a 256th of a bin, is cut by the last slice alone, with bins of the
+// logits' bits over the row: 0.2 ms at 32000 logits, 0.6 at 100000.  Those are
+// rows with runs of equal logits at a cut, as 16-bit ones of large magnitude
+// have, or whose top-k (of thousands) cuts a dense part far below the largest.
+// A row of 150000 logits of one normal distribution, of any mean and any spread
+// from 2^-6 to 100, has fewer than 4096 in every bin.
 //
 // Bound for one row by the three launches and the round trips within them (the
 // last: bins, listing, ticket, list), 22 us at 32000 logits and 29 at 131072; for
@@ -42,20 +47,19 @@ constexpr int kChunk = 8 * kThreads;    // logits a workgroup takes at once
 constexpr int kMaxSlices = 64;
 constexpr uint32_t kRanked = 1024;      // tokens that are ranked by looking at all of them
 constexpr int kList = 4096;             // tokens of the cut bins that are ordered
-constexpr int kBinsPerSign = 68 * 16;   // magnitudes from 2^-5 (below: one bin) to 2^63 (above: one bin)
-constexpr int kBins = 2 * kBinsPerSign;
+constexpr int kBins = 16 * 64;          // distances from the largest logit, from 2^-6 (below: one bin) to 2^10 (above: one bin)
 constexpr int kRowsAtOnce = 1024;       // rows that the workspace has room for
 constexpr int kWeightBits = 38;         // the largest logit's weight is 2^38; 2^24 of them fit in 64 bits
 
 // A row's words in the workspace.
-struct RowWork {
+struct alignas(256) RowWork {
+  uint64_t list[kList];       // key, complement of the index
+  uint64_t mass[kBins];
+  uint32_t count[kBins];
   uint64_t top[kMaxSlices];   // per slice: key, then the complement of the index
   uint64_t best;              // of the race: score key, complement of the index
   uint64_t total;             // weight of the row
   uint32_t listed, arrived;
-  uint64_t list[kList];       // key, complement of the index
-  uint64_t mass[kBins];
-  uint32_t count[kBins];
 };
 
 struct SampleArgs {
@@ -80,14 +84,6 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 
 __device__ __forceinline__ float logit_of(uint32_t key) {
   return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key);
-}
-
-// Bin of a key other than 0: does not fall as the key rises.
-__device__ __forceinline__ int bin_of(uint32_t key) {
-  const bool up = key & 0x80000000u;
-  const uint32_t magnitude = (up ? key : ~key) & 0x7FFFFFFFu;
-  const int i = min(max(static_cast<int>(magnitude >> 19) - ((127 - 5) << 4), 0), kBinsPerSign - 1);
-  return up ? kBinsPerSign + i : kBinsPerSign - 1 - i;
 }
 
 __device__ __forceinline__ uint64_t token_word(uint32_t key, int i) {
@@ -144,6 +140,12 @@ struct Row {
   __device__ __forceinline__ uint64_t weight(uint32_t key) const {
     const uint32_t w = __float_as_uint(relative(key));
     return (static_cast<uint64_t>((w & 0x7FFFFFu) | 0x800000u) << (kWeightBits - 23)) >> min(127u - (w >> 23), 63u);
+  }
+  // Bin of a key other than 0: does not fall as the key rises.  How far the logit
+  // lies below the largest is all that the result depends on.
+  __device__ __forceinline__ int bin(uint32_t key) const {
+    const float d = fmaxf(L - logit_of(key), 0.0f);   // of two infinities: 0
+    return kBins - 1 - min(max(static_cast<int>(__float_as_uint(d) >> 17) - ((127 - 6) << 6), 0), kBins - 1);
   }
   // The race's score of a kept token as a key; 0: not in the race.
   __device__ __forceinline__ uint32_t score(uint32_t key, float noise) const {
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a) {
         const uint64_t m = r.weight(key[i]);
         sum += m;
         if (m >= floor) {
-          const int b = bin_of(key[i]);
+          const int b = r.bin(key[i]);
           atomicAdd(&count[b], 1u);
           atomicAdd(&mass[b], static_cast<unsigned long long>(m));
         }
@@ -293,45 +295,55 @@ struct Cut {
   uint32_t count_above, count;
   uint64_t mass_above, mass;
 };
-// The bins from - tid and their inclusive sums on top of count0 and mass0.
+// A thread's PER bins, from - PER t and those below it, and the sums before and
+// through them on top of count0 and mass0.  The threads hold all bins: from < PER
+// kThreads.
+template <int PER>
 struct Page {
-  uint32_t c, c0;
-  uint64_t m, m0;
+  uint32_t above, through, count[PER];
+  uint64_t mass_above, mass_through, mass[PER];
 };
-template <typename Count, typename Mass>
-__device__ __forceinline__ Page page_of_bins(int from, Count count_at, Mass mass_at, uint32_t count0, uint64_t mass0, Scan& scan) {
-  const int bin = from - static_cast<int>(threadIdx.x);
-  Page g;
-  g.c = g.c0 = bin >= 0 ? count_at(bin) : 0u;
-  g.m = g.m0 = bin >= 0 ? mass_at(bin) : 0u;
-  inclusive(g.c, g.m, scan);
-  g.c += count0, g.m += mass0;
+template <int PER, typename Count, typename Mass>
+__device__ __forceinline__ Page<PER> page_of_bins(int from, Count count_at, Mass mass_at, uint32_t count0, uint64_t mass0, Scan& scan) {
+  Page<PER> g;
+  uint32_t own = 0;
+  uint64_t own_mass = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int bin = from - PER * static_cast<int>(threadIdx.x) - i;
+    g.count[i] = bin >= 0 ? count_at(bin) : 0u;
+    g.mass[i] = bin >= 0 ? mass_at(bin) : 0u;
+    own += g.count[i], own_mass += g.mass[i];
+  }
+  g.through = own, g.mass_through = own_mass;
+  inclusive(g.through, g.mass_through, scan);
+  g.through += count0, g.mass_through += mass0;
+  g.above = g.through - own, g.mass_above = g.mass_through - own_mass;
   return g;
 }
-// first: the page at `from`, which several cuts of the same bins share.
-template <typename Count, typename Mass>
-__device__ __forceinline__ Cut find_cut(int from, Count count_at, Mass mass_at, const Page& first, uint32_t need, double want,
-                                        Scan& scan, Cut& out) {
-  Page g = first;
-  for (int base = from;;) {
-    const int bin = base - static_cast<int>(threadIdx.x);
-    const bool reached = bin >= 0 && (need ? g.c >= need : static_cast<double>(g.m) >= want);
-    // an empty bin reaches a target only where the one before it has; nothing is before the first
-    const bool before = bin != from && (need ? g.c - g.c0 >= need : static_cast<double>(g.m - g.m0) >= want);
-    if (reached && !before) out = Cut{bin, g.c - g.c0, g.c0, g.m - g.m0, g.m0};
-    if (__syncthreads_or(reached)) {
-      const Cut c = out;
-      __syncthreads();   // `out` may be written again
-      return c;
+template <int PER>
+__device__ __forceinline__ Cut find_cut(int from, const Page<PER>& g, uint32_t need, double want, Cut& out) {
+  const int first = from - PER * static_cast<int>(threadIdx.x);
+  auto reaches = [&](uint32_t c, uint64_t m) { return need ? c >= need : static_cast<double>(m) >= want; };
+  // the one thread whose sums go past the target; nothing is before the first bin
+  const bool mine = first >= 0 && reaches(g.through, g.mass_through) && (threadIdx.x == 0 || !reaches(g.above, g.mass_above));
+  if (mine) {
+    uint32_t c = g.above;
+    uint64_t m = g.mass_above;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (!found && reaches(c + g.count[i], m + g.mass[i])) {
+        out = Cut{first - i, c, g.count[i], m, g.mass[i]};
+        found = true;
+      }
+      c += g.count[i], m += g.mass[i];
     }
-    if (threadIdx.x == kThreads - 1) scan.count[0] = g.c, scan.mass[0] = g.m;
-    __syncthreads();
-    const uint32_t cc = scan.count[0];
-    const uint64_t cm = scan.mass[0];
-    base -= kThreads;
-    if (base < 0) return Cut{-1, cc, 0, cm, 0};   // not reached
-    g = page_of_bins(base, count_at, mass_at, cc, cm, scan);
   }
+  const bool any = __syncthreads_or(mine);
+  const Cut cut = any ? out : Cut{-1, 0, 0, 0, 0};   // not reached
+  __syncthreads();   // `out` may be written again
+  return cut;
 }
 
 // What the finish needs of LDS.
@@ -385,7 +397,7 @@ __device__ Cut cut_by_bits(const SampleArgs& a, const T* x, const Row& r, Keep k
     const int from = level == 0 || top >> bits == prefix ? static_cast<int>(top & ((1u << bits) - 1)) : (1 << bits) - 1;
     auto count_at = [&](int b) { return s.bins.count[b]; };
     auto mass_at = [&](int b) { return static_cast<uint64_t>(s.bins.mass[b]); };
-    c = find_cut(from, count_at, mass_at, page_of_bins(from, count_at, mass_at, ca, ma, s.scan), need, want, s.scan, s.cut);
+    c = find_cut(from, page_of_bins<2048 / kThreads>(from, count_at, mass_at, ca, ma, s.scan), need, want, s.cut);
     if (c.bin < 0) break;
     prefix = prefix << bits | static_cast<uint32_t>(c.bin);
     ca = c.count_above, ma = c.mass_above;
@@ -510,7 +522,7 @@ __device__ uint64_t cut_list(const Row& r, uint32_t listed, int bin, uint32_t co
   for (uint32_t i0 = 0; i0 < listed; i0 += kThreads) {
     const uint64_t own = i0 + tid < listed ? s.list[i0 + tid] : 0;
     const uint32_t key = static_cast<uint32_t>(own >> 32);
-    const bool on = own && bin_of(key) == bin;
+    const bool on = own && r.bin(key) == bin;
     const uint32_t to = place(&s.found, on);
     if (on) {
       s.part[to] = own;
@@ -542,8 +554,7 @@ __device__ uint64_t cut_list(const Row& r, uint32_t listed, int bin, uint32_t co
     auto count_at = [&](int b) { return s.count[b]; };
     auto mass_at = [&](int b) { return static_cast<uint64_t>(s.mass[b]); };
     const int from = static_cast<int>((hi - lo) >> shift);
-    const Cut c = find_cut(from, count_at, mass_at, page_of_bins(from, count_at, mass_at, count0, mass0, s.scan), need, want, s.scan,
-                           s.cut);
+    const Cut c = find_cut(from, page_of_bins<1>(from, count_at, mass_at, count0, mass0, s.scan), need, want, s.cut);
     if (tid == 0) s.found = 0;
     __syncthreads();
 #pragma unroll
@@ -592,16 +603,14 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(SampleArgs a) {
   // Bins that the cuts fall into.  Where top-k cuts, the weight that top-p takes
   // its share of lies between the sums above and through its bin, and top-p's cut
   // between the bins of those.
-  auto count_at = [&](int b) { return w.count[b]; };   // written by the launch before
-  auto mass_at = [&](int b) { return w.mass[b]; };
-  const int from = bin_of(r.top);
   Cut by_k{-1, 0, 0, 0, 0}, by_p{-1, 0, 0, 0, 0};
   const bool cuts = r.k || r.p < 1.0f;   // the same for the whole row
   const uint64_t total = r.p < 1.0f ? w.total : 0;
-  const Page first = cuts ? page_of_bins(from, count_at, mass_at, 0u, 0u, s.scan) : Page{};
-  auto cut_at = [&](uint32_t need, double of) {
-    return find_cut(from, count_at, mass_at, first, need, static_cast<double>(r.p) * of, s.scan, s.cut);
-  };
+  Page<kBins / kThreads> bins = {};
+  if (cuts)   // written by the launch before
+    bins = page_of_bins<kBins / kThreads>(
+        kBins - 1, [&](int b) { return w.count[b]; }, [&](int b) { return w.mass[b]; }, 0u, 0u, s.scan);
+  auto cut_at = [&](uint32_t need, double of) { return find_cut(kBins - 1, bins, need, static_cast<double>(r.p) * of, s.cut); };
   if (r.k) by_k = cut_at(static_cast<uint32_t>(r.k), 0.0);
   int p_low = -1, high = by_k.bin;
   if (r.p < 1.0f) {
@@ -632,7 +641,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(SampleArgs a) {
     if (at0 + kChunk < end) load_keys8(x, min(at + kChunk, end), end, next);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int b = key[i] ? bin_of(key[i]) : -2;
+      const int b = key[i] ? r.bin(key[i]) : -2;
       if (b > high) {   // passes both
         if (key[i]) race(key[i], at + i, [&] { return cuts ? noise[at + i] : e[i]; });
       }

@@ -20,3 +20,50 @@ def test_top_p_that_keeps_the_first_token_alone(env, p):  # noqa: F811
                 got = _sample(env, x, noise, **f)
                 assert (got == x.float().cpu().numpy().argmax(1)).all(), (dtype, f)
                 assert (got == _want(x, noise, **f)).all()
+
+
+def _offset_rows(torch, rows, V, offset, dtype, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    logits = (offset + 2 * torch.randn(rows, V, generator=g, device="cuda")).to(dtype)
+    return logits, torch.empty(rows, V, device="cuda").exponential_(generator=g)
+
+
+OFFSETS = [0.0, 8.0, 20.0, -20.0, -40.0, 300.0, -1000.0]
+
+
+@pytest.mark.parametrize("offset", OFFSETS)
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+def test_logits_with_an_offset(env, offset, dtype):  # noqa: F811
+    """The token depends on differences of logits only; so does how it is found."""
+    torch, _ = env
+    for V in (5001, 32000, 100277):
+        logits, noise = _offset_rows(torch, 2, V, offset, getattr(torch, dtype), V)
+        for f in (dict(p=0.9), dict(p=0.5, T=1.7), dict(k=400, p=0.9), dict(k=3000), dict(k=3000, p=0.97, T=0.4), dict(p=0.99, m=1e-4)):
+            assert (_sample(env, logits, noise, **f) == _want(logits, noise, **f)).all(), (V, f)
+
+
+@pytest.mark.parametrize("offset", OFFSETS[1:])
+@pytest.mark.parametrize("V", [32000, 100277])
+def test_an_offset_does_not_change_the_time(env, offset, V):  # noqa: F811
+    """Rows without runs of equal logits are cut from a list of a few thousand
+    tokens at most, wherever they lie; one workgroup alone takes 20 times as long."""
+    torch, celty = env
+    p = torch.full((2,), 0.9, device="cuda")
+    tokens = torch.empty(2, dtype=torch.int32, device="cuda")
+
+    def best_time(at):
+        logits, noise = _offset_rows(torch, 2, V, at, torch.float32, 43)
+        ws = celty.new_sample_workspace(logits)
+        times = []
+        for _ in range(8):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(10):
+                celty.celty_sample(logits, noise, tokens, ws, top_p=p)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    plain = best_time(0.0)
+    assert best_time(offset) < 4 * plain
