@@ -208,7 +208,7 @@ typedef struct celty_filters {
  *           ldl >= V.  NaN and -infinity are never chosen; where +infinity
  *           occurs, only those tokens have weight.
  *   noise   device fp32, rows x V, row stride ldn >= V; read only where a
- *           token is kept.  Values below 2^-126 count as 2^-126, NaN as
+ *           token is kept, in a row without top_k, top_p and min_p everywhere.  Values below 2^-126 count as 2^-126, NaN as
  *           +infinity.  May be NULL: every row takes its largest logit.
  *   tokens  device int32[rows]; -1 for a row with no number to choose.
  * Weights are summed as multiples of 2^-38 of the largest, in 64-bit integers:

@@ -604,7 +604,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(SampleArgs a) {
   // its share of lies between the sums above and through its bin, and top-p's cut
   // between the bins of those.
   Cut by_k{-1, 0, 0, 0, 0}, by_p{-1, 0, 0, 0, 0};
-  const bool cuts = r.k || r.p < 1.0f;   // the same for the whole row
+  const bool cuts = r.k || r.p < 1.0f, all = !cuts && !(r.min_p > 0.0f);   // the same for the whole row
   const uint64_t total = r.p < 1.0f ? w.total : 0;
   Page<kBins / kThreads> bins = {};
   if (cuts)   // written by the launch before
@@ -637,13 +637,13 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(SampleArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) key[i] = next[i];
     float e[8];
-    if (!cuts) load8(noise + min(at, end), end - at, e);   // all of it is needed
+    if (all) load8(noise + min(at, end), end - at, e);   // every number races
     if (at0 + kChunk < end) load_keys8(x, min(at + kChunk, end), end, next);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int b = key[i] ? r.bin(key[i]) : -2;
       if (b > high) {   // passes both
-        if (key[i]) race(key[i], at + i, [&] { return cuts ? noise[at + i] : e[i]; });
+        if (key[i]) race(key[i], at + i, [&] { return all ? e[i] : noise[at + i]; });
       }
       const bool on = b <= high && b >= 0 && (b == by_k.bin || (p_low >= 0 && b >= p_low));
       const uint32_t to = place(&s.listed, on);   // in any order: the list is ordered below
