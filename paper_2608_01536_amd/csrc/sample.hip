@@ -17,11 +17,11 @@
 //           the slice that arrives last orders the list (some dozens of
 //           tokens), cuts it exactly and lets the rest race.
 //
-// A row whose cut bins hold more tokens than the list does (4096), or more than
-// 1024 in a 256th of a bin, is cut by the last slice alone, with bins of the
-// logits' bits over the row: 0.2 ms at 32000 logits, 0.6 at 100000.  Those are
-// rows with runs of equal logits at a cut, as 16-bit ones of large magnitude
-// have, or whose top-k (of thousands) cuts a dense part far below the largest.
+// A row whose cut bins hold more tokens than the list does (4096) is cut by the
+// last slice alone, with bins of the logits' bits over the row: 0.2 ms at 32000
+// logits, 0.6 at 100000.  Those are rows with thousands of equal logits at a cut,
+// as 16-bit ones of large magnitude have, or whose top-k (of thousands) cuts a
+// dense part far below the largest.
 // A row of 150000 logits of one normal distribution, of any mean and any spread
 // from 2^-6 to 100, has fewer than 4096 in every bin.
 //
@@ -45,8 +45,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kChunk = 8 * kThreads;    // logits a workgroup takes at once
 constexpr int kMaxSlices = 64;
-constexpr uint32_t kRanked = 1024;      // tokens that are ranked by looking at all of them
-constexpr int kList = 4096;             // tokens of the cut bins that are ordered
+constexpr int kList = 4096;             // tokens of the cut bins that a cut is found among
 constexpr int kBins = 16 * 64;          // distances from the largest logit, from 2^-6 (below: one bin) to 2^10 (above: one bin)
 constexpr int kRowsAtOnce = 1024;       // rows that the workspace has room for
 constexpr int kWeightBits = 38;         // the largest logit's weight is 2^38; 2^24 of them fit in 64 bits
@@ -351,11 +350,11 @@ struct FinishLds {
   Scan scan;
   Cut cut;
   uint64_t best[kThreads / kWave], word;
-  uint32_t lo[kThreads / kWave], hi[kThreads / kWave];
+  uint64_t lo[kThreads / kWave], hi[kThreads / kWave];
   uint32_t base, listed, found;
   union {
     struct {
-      uint64_t list[kList], part[kList], weight[kRanked];
+      uint64_t list[kList], few[kWave];
       unsigned long long mass[kThreads];
       uint32_t count[kThreads];
     };
@@ -510,73 +509,61 @@ __device__ uint64_t finish_row(const SampleArgs& a, const T* x, const float* noi
 // The cut among the listed tokens of one bin, whose tokens come after the
 // sums count0 and mass0: the word of the last kept token (need > 0: the one that
 // makes the count, else the one that makes the weight), and the weight up to it.
-// 0 where more tokens than kRanked share a 256th of the bin.
+// The bin's sums reach the target, so there is one.
 __device__ uint64_t cut_list(const Row& r, uint32_t listed, int bin, uint32_t count0, uint64_t mass0, uint32_t need, double want,
                              uint64_t& upto, FinishLds& s) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
-  __syncthreads();
-  if (tid == 0) s.found = 0, s.word = 0;
-  s.mass[tid] = 0, s.count[tid] = 0;
-  __syncthreads();
-  uint32_t lo = 0xFFFFFFFFu, hi = 0;
-  for (uint32_t i0 = 0; i0 < listed; i0 += kThreads) {
-    const uint64_t own = i0 + tid < listed ? s.list[i0 + tid] : 0;
-    const uint32_t key = static_cast<uint32_t>(own >> 32);
-    const bool on = own && r.bin(key) == bin;
-    const uint32_t to = place(&s.found, on);
-    if (on) {
-      s.part[to] = own;
-      lo = min(lo, key), hi = max(hi, key);
+  uint64_t from = 0, to = ~0ull;   // the bin's tokens that may be the last kept
+  uint32_t n;
+  for (;;) {
+    __syncthreads();
+    if (tid == 0) s.found = 0;
+    s.mass[tid] = 0, s.count[tid] = 0;
+    __syncthreads();
+    uint64_t lo = ~0ull, hi = 0;
+    for (uint32_t i0 = 0; i0 < listed; i0 += kThreads) {
+      const uint64_t own = i0 + tid < listed ? s.list[i0 + tid] : 0;
+      const bool on = own && own >= from && own <= to && r.bin(static_cast<uint32_t>(own >> 32)) == bin;
+      const uint32_t at = place(&s.found, on);
+      if (on) {
+        if (at < kWave) s.few[at] = own;
+        lo = own < lo ? own : lo, hi = own > hi ? own : hi;
+      }
     }
-  }
-  __syncthreads();
-  uint32_t n = s.found;
-  if (n > kWave) {
-    // 256 bins of the tokens' own range leave few
-    lo = ~wave_max(~lo), hi = wave_max(hi);
+    lo = ~wave_max<unsigned long long>(~lo), hi = wave_max<unsigned long long>(hi);
     if (lane == 0) s.lo[wv] = lo, s.hi[wv] = hi;
     __syncthreads();
+    n = s.found;
+    if (n <= kWave) break;
+    // 256 bins of the words' own range, whose low half orders equal logits, leave
+    // few; no two words are equal, so that at last each has a bin of its own
 #pragma unroll
-    for (int i = 0; i < kThreads / kWave; ++i) lo = min(lo, s.lo[i]), hi = max(hi, s.hi[i]);
-    const int shift = max(24 - __builtin_clz((hi - lo) | 1u), 0);
-    uint64_t word[kList / kThreads];
-#pragma unroll
-    for (int u = 0; u < kList / kThreads; ++u) {
-      const uint32_t i = tid + u * kThreads;
-      word[u] = i < n ? s.part[i] : 0;
-      if (word[u]) {
-        const uint32_t key = static_cast<uint32_t>(word[u] >> 32), b = (key - lo) >> shift;
+    for (int i = 0; i < kThreads / kWave; ++i) lo = s.lo[i] < lo ? s.lo[i] : lo, hi = s.hi[i] > hi ? s.hi[i] : hi;
+    const int shift = max(56 - __builtin_clzll((hi - lo) | 1u), 0);
+    for (uint32_t i = tid; i < listed; i += kThreads) {
+      const uint64_t own = s.list[i];
+      if (own >= lo && own <= hi) {
+        const int b = static_cast<int>((own - lo) >> shift);
         atomicAdd(&s.count[b], 1u);
-        atomicAdd(&s.mass[b], static_cast<unsigned long long>(r.weight(key)));
+        atomicAdd(&s.mass[b], static_cast<unsigned long long>(r.weight(static_cast<uint32_t>(own >> 32))));
       }
     }
     __syncthreads();
-    auto count_at = [&](int b) { return s.count[b]; };
-    auto mass_at = [&](int b) { return static_cast<uint64_t>(s.mass[b]); };
-    const int from = static_cast<int>((hi - lo) >> shift);
-    const Cut c = find_cut(from, page_of_bins<1>(from, count_at, mass_at, count0, mass0, s.scan), need, want, s.cut);
-    if (tid == 0) s.found = 0;
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kList / kThreads; ++u) {
-      const bool on = word[u] && static_cast<int>((static_cast<uint32_t>(word[u] >> 32) - lo) >> shift) == c.bin;
-      const uint32_t to = place(&s.found, on);
-      if (on) s.part[to] = word[u];
-    }
-    __syncthreads();
-    n = s.found, count0 = c.count_above, mass0 = c.mass_above;
+    const int top = static_cast<int>((hi - lo) >> shift);
+    const Cut c = find_cut(top, page_of_bins<1>(top, [&](int b) { return s.count[b]; },
+                                                [&](int b) { return static_cast<uint64_t>(s.mass[b]); }, count0, mass0, s.scan),
+                           need, want, s.cut);
+    from = lo + (static_cast<uint64_t>(c.bin) << shift), to = from + ((1ull << shift) - 1);
+    count0 = c.count_above, mass0 = c.mass_above;
   }
-  if (n > kRanked) return 0;
-  for (uint32_t t = tid; t < n; t += kThreads) s.weight[t] = r.weight(static_cast<uint32_t>(s.part[t] >> 32));
-  __syncthreads();
   // what comes before a token, by looking at all
-  for (uint32_t t = tid; t < n; t += kThreads) {
-    const uint64_t own = s.part[t];
+  if (tid < static_cast<int>(n)) {
+    const uint64_t own = s.few[tid];
     uint32_t rank = count0;
     uint64_t before = mass0;
     for (uint32_t i = 0; i < n; ++i)
-      if (s.part[i] > own) ++rank, before += s.weight[i];
-    const uint64_t after = before + s.weight[t];
+      if (s.few[i] > own) ++rank, before += r.weight(static_cast<uint32_t>(s.few[i] >> 32));
+    const uint64_t after = before + r.weight(static_cast<uint32_t>(own >> 32));
     // of the weight's cut: the last token with less than `want` before it, at least the first
     const bool last = need ? rank == need - 1
                            : static_cast<double>(after) >= want && (static_cast<double>(before) < want || rank == 0);
@@ -684,27 +671,19 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(SampleArgs a) {
     best = finish_row(a, x, noise, r, s);
   } else if (listed) {
     uint64_t cut = 0, upto = total;   // listed tokens from this word up are kept
-    bool ranked = true;
-    if (by_k.bin >= 0) {
+    if (by_k.bin >= 0)
       cut = cut_list(r, listed, by_k.bin, by_k.count_above, by_k.mass_above, static_cast<uint32_t>(r.k), 0.0, upto, s);
-      ranked = cut != 0;
-    }
-    if (ranked && r.p < 1.0f) {
+    if (r.p < 1.0f) {
       const double of = static_cast<double>(upto);
       if (by_k.bin >= 0) {
         __syncthreads();
         by_p = cut_at(0u, of);
       }
       const uint64_t c = cut_list(r, listed, by_p.bin, by_p.count_above, by_p.mass_above, 0u, static_cast<double>(r.p) * of, upto, s);
-      ranked = c != 0;
       cut = c > cut ? c : cut;
     }
-    if (ranked) {
-      for (uint32_t i = tid; i < listed; i += kThreads)
-        if (s.list[i] >= cut) race(static_cast<uint32_t>(s.list[i] >> 32), index_of(s.list[i]), [&] { return noise[index_of(s.list[i])]; });
-    } else {
-      best = finish_row(a, x, noise, r, s);   // more than a thousand tokens within one part of a bin
-    }
+    for (uint32_t i = tid; i < listed; i += kThreads)
+      if (s.list[i] >= cut) race(static_cast<uint32_t>(s.list[i] >> 32), index_of(s.list[i]), [&] { return noise[index_of(s.list[i])]; });
   }
   best = block_best(best, s);
   if (tid == 0) a.tokens[row] = index_of(best);
@@ -716,7 +695,7 @@ struct SamplePlan {
 
 // One chunk a slice where the rows alone do not fill the compute units, four
 // where they do; kMaxSlices of a row at most.  The finish keeps two workgroups a
-// unit (its lists take 76 KB of LDS) busy for one round.
+// unit busy for one round.
 SamplePlan make_plan(int32_t rows, int32_t V) {
   const int chunks = (V + kChunk - 1) / kChunk, n = std::min(rows, kRowsAtOnce);
   int per = static_cast<int64_t>(n) * chunks > 2048 ? 4 : 1;

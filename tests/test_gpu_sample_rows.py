@@ -67,3 +67,53 @@ def test_an_offset_does_not_change_the_time(env, offset, V):  # noqa: F811
         return min(times)
     plain = best_time(0.0)
     assert best_time(offset) < 4 * plain
+
+
+@pytest.mark.parametrize("dtype,offset", [("bfloat16", 8.0), ("bfloat16", 20.0), ("bfloat16", -20.0), ("float16", -40.0), ("float16", 100.0)])
+def test_equal_logits_in_thousands_do_not_change_the_time(env, dtype, offset):  # noqa: F811
+    """16-bit logits with an offset are runs of equal ones, up to two thousand here."""
+    torch, celty = env
+    V = 100277
+    p = torch.full((2,), 0.9, device="cuda")
+    tokens = torch.empty(2, dtype=torch.int32, device="cuda")
+
+    def best_time(at):
+        logits, noise = _offset_rows(torch, 2, V, at, getattr(torch, dtype), 44)
+        ws = celty.new_sample_workspace(logits)
+        times = []
+        for _ in range(8):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(10):
+                celty.celty_sample(logits, noise, tokens, ws, top_p=p)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    plain = best_time(0.0)
+    assert best_time(offset) < 3 * plain
+
+
+@pytest.mark.parametrize("run", [65, 300, 1025, 2000, 4096, 4097, 9000])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_cuts_within_runs_of_equal_logits(env, run, dtype):  # noqa: F811
+    """Runs below a few larger logits, spread over the row or side by side, one
+    near another: the lower indices are kept."""
+    torch, _ = env
+    V = 20011
+    g = torch.Generator(device="cuda")
+    g.manual_seed(run)
+    x = torch.full((6, V), -30.0, device="cuda")
+    for r in range(6):
+        at = torch.randperm(V, generator=g, device="cuda")[:run] if r % 2 else torch.arange(700, 700 + run, device="cuda")
+        x[r, at] = 3.0
+        more = torch.randperm(V, generator=g, device="cuda")[:30]
+        x[r, more[:20]] = 3.0 + 0.25 * torch.arange(20, device="cuda") / (1 + r)
+        x[r, more[20:]] = 2.984375
+    x = x.to(getattr(torch, dtype))
+    noise = torch.empty(6, V, device="cuda").exponential_(generator=g)
+    one = torch.ones_like(noise)
+    one[:, ::7] = 0.5
+    for f in (dict(k=21), dict(k=run // 2), dict(k=run + 9), dict(k=run + 25), dict(p=0.3), dict(p=0.9), dict(k=run - 1, p=0.7), dict(k=40, p=0.999)):
+        for e in (noise, one):
+            assert (_sample(env, x, e, **f) == _want(x, e, **f)).all(), f
