@@ -108,6 +108,21 @@ def _gpu(t, name: str) -> int:
     return dev
 
 
+def _stream_on(stream, dev: int) -> int:
+    """The stream's handle.  A launch goes to the current GPU, so that must be
+    the tensors', and a given stream's as well."""
+    c = _torch()._C
+    current = c._cuda_getDevice()
+    if current != dev:
+        raise ValueError(f"the call's tensors are on cuda:{dev}, the current device is cuda:{current}")
+    if stream is None:
+        return c._cuda_getCurrentRawStream(dev)   # without a stream object, as _stream_handle
+    given = getattr(stream, "device", None)
+    if given is not None and given.index is not None and given.index != dev:
+        raise ValueError(f"the call's tensors are on cuda:{dev}, its stream on {given}")
+    return _stream_handle(stream)
+
+
 def celty_block_norm(h, b, h_out=None, x=None, *, kind: str = "rms", w_pre=None, b_pre=None, w_post=None, b_post=None,
                      gate=None, alpha: float = 1.0, eps: float = 1e-5, post: Optional[bool] = None, stream=None) -> None:
     """h_out = h + alpha * gate * u and x = norm(h_out) * w_pre + b_pre, with
@@ -144,7 +159,7 @@ def celty_block_norm(h, b, h_out=None, x=None, *, kind: str = "rms", w_pre=None,
     a = celty_norm(_NORM_KINDS[kind], w_post is not None if post is None else bool(post), eps, alpha,
                    _vector(w_pre, n, dtype, dev, "w_pre"), _vector(b_pre, n, dtype, dev, "b_pre"),
                    _vector(w_post, n, dtype, dev, "w_post"), _vector(b_post, n, dtype, dev, "b_post"), gp, ldg)
-    status = _norm(rows, n, a, code, res, hp, ldh, bp, ldb, op, ldo, xp, ldx, _stream_handle(stream))
+    status = _norm(rows, n, a, code, res, hp, ldh, bp, ldb, op, ldo, xp, ldx, _stream_on(stream, dev))
     if status:
         _check(status, "celty_block_norm")
 
@@ -247,7 +262,7 @@ def _move(f, where, cache: Kv4Cache, seqs: Kv4Seqs, k, v, stream):
     kh = _heads(k, cache.kv_heads, cache, "k")
     vh = _heads(v, cache.kv_heads, cache, "v", k)
     _same_gpu(cache, seqs)
-    status = f(cache._desc, seqs.desc(k.size(0)), _dtype_code(k.dtype, "k"), kh, vh, _stream_handle(stream))
+    status = f(cache._desc, seqs.desc(k.size(0)), _dtype_code(k.dtype, "k"), kh, vh, _stream_on(stream, cache._dev))
     if status:
         _check(status, where)
 
@@ -287,7 +302,7 @@ def celty_kv4_attention(cache: Kv4Cache, seqs: Kv4Seqs, q, out, workspace, scale
         scale = 1.0 / math.sqrt(cache.head_dim)
     status = _attention(cache._desc, seqs.desc(q.size(0)), _dtype_code(q.dtype, "q"), q.size(1), qh, oh, scale, window,
                         _vector(workspace, 0, _torch().uint8, cache._dev, "workspace"), workspace.numel(),
-                        _stream_handle(stream))
+                        _stream_on(stream, cache._dev))
     if status:
         _check(status, "celty_kv4_attention")
 
@@ -320,7 +335,7 @@ def celty_sample(logits, noise, tokens, workspace, temperature=None, top_k=None,
                       _vector(top_p, rows, torch.float32, dev, "top_p"), _vector(min_p, rows, torch.float32, dev, "min_p"))
     status = _sample(rows, V, _dtype_code(logits.dtype, "logits", _FLOATS), lp, ldl, np_, ldn, f,
                      _vector(tokens, rows, torch.int32, dev, "tokens"), _vector(workspace, 0, torch.uint8, dev, "workspace"),
-                     workspace.numel(), _stream_handle(stream))
+                     workspace.numel(), _stream_on(stream, dev))
     if status:
         _check(status, "celty_sample")
 
