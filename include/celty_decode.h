@@ -64,8 +64,9 @@ typedef struct celty_norm {
  *   h, b, h_out, x   device, row strides ldh, ldb, ldho, ldx (elements, >= n),
  *              aligned to their element.  b NULL: no update (u = 0).  h_out
  *              NULL: not written; x NULL: not written (one of them is
- *              needed).  h_out may be h, and x may be b; any other overlap of
- *              an output with another operand is not allowed.
+ *              needed).  h_out may be h, and x may be b; any other element
+ *              that an output shares with another operand is refused (rows
+ *              beside each other in one larger matrix share none).
  * rows = 0 does nothing.
  * Errors: EINVAL (null h or norm, both outputs null, rows < 0, n < 1, bad kind
  *         or dtype, eps not positive and finite, NaN alpha, short stride,
@@ -123,8 +124,9 @@ typedef struct celty_kv4_seqs {
 
 /* A [n_tokens][heads][D] tensor in device memory: strides in elements, the
  * channels contiguous, the pointer aligned to 16 bytes and the strides multiples
- * of 8; at least D in a tensor that is written (a stride along one element is of
- * no matter). */
+ * of 8; at least D in a tensor that is written, whose rows of D channels may not
+ * share elements with each other or with another operand (a stride along one
+ * element is of no matter). */
 typedef struct celty_heads {
   void* data;
   int64_t token_stride;

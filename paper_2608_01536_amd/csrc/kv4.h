@@ -113,6 +113,11 @@ inline celty_status check_heads(const celty_heads* t, int32_t n_tokens, int32_t 
   return CELTY_OK;
 }
 
+// The rows of D channels of a tensor that the checks above let pass.
+inline Rows rows_of(const celty_heads* t, int32_t n_tokens, int32_t heads, int32_t D) {
+  return {t->data, n_tokens, 2 * t->token_stride, heads, 2 * t->head_stride, 2 * int64_t{D}};
+}
+
 inline Kv4Args make_args(const celty_kv4_cache* c, const celty_kv4_seqs* s) {
   Kv4Args a;
   a.k_codes = c->k_codes;

@@ -252,6 +252,10 @@ celty_status move_tokens(bool append, const celty_kv4_cache* c, const celty_kv4_
   if (check_heads(k, s->n_tokens, c->kv_heads, out) != CELTY_OK || check_heads(v, s->n_tokens, c->kv_heads, out) != CELTY_OK)
     return CELTY_EINVAL;
   if (s->n_tokens == 0 || s->n_seqs == 0) return CELTY_OK;
+  if (!append) {
+    const Rows kr = rows_of(k, s->n_tokens, c->kv_heads, c->head_dim), vr = rows_of(v, s->n_tokens, c->kv_heads, c->head_dim);
+    if (!rows_apart(kr) || !rows_apart(vr) || rows_overlap(kr, vr)) return CELTY_EINVAL;
+  }
   // at most n / 8 + 2 octets for a sequence's n tokens
   const int64_t octets = s->q_start ? s->n_tokens / 8 + 2 * static_cast<int64_t>(s->n_seqs) : s->n_seqs;
   const int64_t units = octets * c->kv_heads;

@@ -921,10 +921,8 @@ extern "C" celty_status celty_kv4_attention(const celty_kv4_cache* cache, const 
   const Plan plan = make_plan(cache, seqs, heads);
   if (!workspace || misaligned(workspace, 256) || workspace_bytes < plan.bytes) return CELTY_EINVAL;
   if (seqs->n_tokens == 0 || seqs->n_seqs == 0) return CELTY_OK;
-  auto span = [&](const celty_heads* t) {
-    return 2 * static_cast<uint64_t>((seqs->n_tokens - 1) * t->token_stride + (heads - 1) * t->head_stride + cache->head_dim);
-  };
-  if (ranges_overlap(q->data, span(q), out->data, span(out))) return CELTY_EINVAL;
+  const Rows qr = rows_of(q, seqs->n_tokens, heads, cache->head_dim), outr = rows_of(out, seqs->n_tokens, heads, cache->head_dim);
+  if (!rows_apart(outr) || rows_overlap(qr, outr)) return CELTY_EINVAL;
   const Kv4Args a = make_args(cache, seqs);
   const AttnArgs f{q->data, out->data, q->token_stride, q->head_stride, out->token_stride, out->head_stride,
                    heads / cache->kv_heads, scale * 1.44269504088896341f, window, plan.n_splits, plan.tiles_per_seq, static_cast<int>(plan.tiles),

@@ -250,9 +250,7 @@ void launch_norm(NormArgs a, int rows, hipStream_t st) {
   a.n % 8 ? shaped(std::true_type{}) : shaped(std::false_type{});
 }
 
-uint64_t span_bytes(int rows, int n, int64_t ld, int size) {
-  return (static_cast<uint64_t>(rows - 1) * static_cast<uint64_t>(ld) + static_cast<uint64_t>(n)) * static_cast<uint64_t>(size);
-}
+Rows rows_of(const void* p, int rows, int n, int64_t ld, int size) { return {p, ld ? rows : 1, ld * size, 1, 0, int64_t{1} * n * size}; }
 
 }  // namespace
 
@@ -281,17 +279,18 @@ extern "C" celty_status celty_block_norm(int32_t rows, int32_t n, const celty_no
     if (misaligned(p, 2)) return CELTY_EINVAL;
   if (misaligned(h, rs) || misaligned(h_out, rs)) return CELTY_EINVAL;
   // an output may only be the operand it replaces, row for row
-  const uint64_t hb = span_bytes(rows, n, ldh, rs), bb = b ? span_bytes(rows, n, ldb, 2) : 0;
-  const uint64_t ob = h_out ? span_bytes(rows, n, ldho, rs) : 0, xb = x ? span_bytes(rows, n, ldx, 2) : 0;
-  const uint64_t nb = 2 * static_cast<uint64_t>(n);
-  const uint64_t gb = norm->gate ? (norm->ld_gate ? span_bytes(rows, n, norm->ld_gate, 2) : nb) : 0;
-  const bool h_in_place = h_out == h && ldho == ldh, b_in_place = x == b && ldx == ldb;
-  if (ranges_overlap(h_out, ob, x, xb)) return CELTY_EINVAL;
-  if ((!h_in_place && ranges_overlap(h_out, ob, h, hb)) || ranges_overlap(h_out, ob, b, bb)) return CELTY_EINVAL;
-  if ((!b_in_place && ranges_overlap(x, xb, b, bb)) || ranges_overlap(x, xb, h, hb)) return CELTY_EINVAL;
-  for (const void* p : {norm->w_pre, norm->b_pre, norm->w_post, norm->b_post})
-    if (ranges_overlap(h_out, ob, p, nb) || ranges_overlap(x, xb, p, nb)) return CELTY_EINVAL;
-  if (ranges_overlap(h_out, ob, norm->gate, gb) || ranges_overlap(x, xb, norm->gate, gb)) return CELTY_EINVAL;
+  const Rows hr = rows_of(h, rows, n, ldh, rs), br = rows_of(b, rows, n, ldb, 2);
+  const Rows outr = rows_of(h_out, rows, n, ldho, rs), xr = rows_of(x, rows, n, ldx, 2);
+  const bool h_in_place = h_out == h && (ldho == ldh || rows == 1), b_in_place = x == b && (ldx == ldb || rows == 1);
+  if (rows_overlap(outr, xr)) return CELTY_EINVAL;
+  if ((!h_in_place && rows_overlap(outr, hr)) || rows_overlap(outr, br)) return CELTY_EINVAL;
+  if ((!b_in_place && rows_overlap(xr, br)) || rows_overlap(xr, hr)) return CELTY_EINVAL;
+  for (const void* p : {norm->w_pre, norm->b_pre, norm->w_post, norm->b_post}) {
+    const Rows vector = rows_of(p, 1, n, n, 2);
+    if (rows_overlap(outr, vector) || rows_overlap(xr, vector)) return CELTY_EINVAL;
+  }
+  const Rows gr = rows_of(norm->gate, rows, n, norm->ld_gate, 2);
+  if (rows_overlap(outr, gr) || rows_overlap(xr, gr)) return CELTY_EINVAL;
 
   const NormArgs a{n,          norm->kind == CELTY_NORM_LAYER, norm->post, norm->eps,     norm->alpha, norm->w_pre,
                    norm->b_pre, norm->w_post, norm->b_post, norm->gate, norm->ld_gate, h, b, h_out, x, ldh, ldb, ldho, ldx, 0};

@@ -171,3 +171,35 @@ def test_queries_that_are_not_finite(env, which, bad, positive):  # noqa: F811
     assert got[row, h].isnan().all()
     got[row, h] = out[row, h]
     assert torch.equal(got, out)
+
+
+def test_queries_and_results_beside_each_other(env):  # noqa: F811
+    """One tensor that holds both: whole heads side by side, and head by head."""
+    torch, celty = env
+    s = Sequences(env, [70, 33], [20, 3], 2, 64, 32, "float16", seed=37)
+    s.fill()
+    q, out, ws = _attend(env, s, 4)
+    for shape, parts in (((23, 8, 64), lambda t: (t[:, :4], t[:, 4:])), ((23, 4, 2, 64), lambda t: (t[:, :, 0], t[:, :, 1])),
+                         ((4, 23, 2, 64), lambda t: (t[:, :, 0].permute(1, 0, 2), t[:, :, 1].permute(1, 0, 2)))):
+        both = torch.full(shape, 7.0, dtype=torch.float16, device="cuda")
+        qv, ov = parts(both)
+        qv.copy_(q)
+        celty.celty_kv4_attention(s.cache, s.seqs, qv, ov, ws)
+        assert torch.equal(ov, out) and torch.equal(qv, q)
+    kv = torch.empty(23, 2, 2, 64, dtype=torch.float16, device="cuda")
+    celty.celty_kv4_gather(s.cache, s.seqs, kv[:, 0], kv[:, 1])
+    k, v = torch.empty_like(kv[:, 0]), torch.empty_like(kv[:, 0])
+    celty.celty_kv4_gather(s.cache, s.seqs, k, v)
+    assert torch.equal(kv[:, 0], k) and torch.equal(kv[:, 1], v)
+
+
+def test_norm_operands_beside_each_other(env):  # noqa: F811
+    torch, celty = env
+    h, b = torch.randn(9, 100, device="cuda").half(), torch.randn(9, 100, device="cuda").half()
+    w = torch.rand(100, device="cuda").half()
+    h_out, x = torch.empty_like(h), torch.empty_like(h)
+    celty.celty_block_norm(h, b, h_out, x, w_pre=w)
+    one = torch.zeros(9, 4, 100, dtype=torch.float16, device="cuda")
+    one[:, 0], one[:, 1] = h, b
+    celty.celty_block_norm(one[:, 0], one[:, 1], one[:, 2], one[:, 3], w_pre=w)
+    assert torch.equal(one[:, 0], h) and torch.equal(one[:, 1], b) and torch.equal(one[:, 2], h_out) and torch.equal(one[:, 3], x)
