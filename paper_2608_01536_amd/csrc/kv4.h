@@ -107,15 +107,15 @@ inline celty_status check_cache_pointers(const celty_kv4_cache* c, const celty_k
 // least: the smallest stride that keeps a tensor's rows apart, for one that is written; else 0.
 inline celty_status check_heads(const celty_heads* t, int32_t n_tokens, int32_t heads, int32_t least) {
   if (!t || (n_tokens && !t->data) || misaligned(t->data, 16)) return CELTY_EINVAL;
-  if (t->token_stride < 0 || t->head_stride < 0 || t->token_stride % 8 || t->head_stride % 8) return CELTY_EINVAL;
-  if ((n_tokens > 1 && t->token_stride < least) || (heads > 1 && t->head_stride < least)) return CELTY_EINVAL;
-  if (t->token_stride > (int64_t{1} << 31) || t->head_stride > (int64_t{1} << 31)) return CELTY_EINVAL;
-  return CELTY_OK;
+  auto stride_ok = [&](int64_t stride, int32_t count) {   // one along a single element is not looked at
+    return count <= 1 || (stride >= least && stride >= 0 && stride % 8 == 0 && stride <= int64_t{1} << 31);
+  };
+  return stride_ok(t->token_stride, n_tokens) && stride_ok(t->head_stride, heads) ? CELTY_OK : CELTY_EINVAL;
 }
 
 // The rows of D channels of a tensor that the checks above let pass.
 inline Rows rows_of(const celty_heads* t, int32_t n_tokens, int32_t heads, int32_t D) {
-  return {t->data, n_tokens, 2 * t->token_stride, heads, 2 * t->head_stride, 2 * int64_t{D}};
+  return {t->data, n_tokens, n_tokens > 1 ? 2 * t->token_stride : 0, heads, heads > 1 ? 2 * t->head_stride : 0, 2 * int64_t{D}};
 }
 
 inline Kv4Args make_args(const celty_kv4_cache* c, const celty_kv4_seqs* s) {

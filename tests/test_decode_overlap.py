@@ -104,3 +104,16 @@ def test_norm_of_columns_of_one_buffer(res):
     assert call(0, wh, far, far + wh) and call(0, wh, far + wx, far)
     assert not call(0, wh, far, far + ld - 2)                      # x ends in the next row's h_out
     assert call(0, wh, far, far + ld - wx)
+
+
+@host_only
+def test_a_stride_along_one_element_is_of_no_matter():
+    odd = 12345
+    for n, heads, a, b in ((1, 4, (FAKE, odd, 64), (FAKE + 0x100000, -odd, 64)), (3, 1, (FAKE, 64, odd), (FAKE + 0x100000, 64, 0)),
+                           (1, 1, (FAKE, 1 << 40, -3), (FAKE + 0x100000, 5, 1 << 50))):
+        seqs = _seqs(n_tokens=n)
+        c = _cache(head_dim=64, kv_heads=heads)
+        x, y = decode.celty_heads(*a), decode.celty_heads(*b)
+        for f in (decode._append, decode._gather):
+            assert f(B(c), B(seqs), F16, B(x), B(y), None) != CELTY_EINVAL, (n, heads)
+        assert decode._attention(B(c), B(seqs), F16, heads, B(x), B(y), 0.1, 0, WS, 1 << 40, None) != CELTY_EINVAL, (n, heads)
