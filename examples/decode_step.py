@@ -122,7 +122,8 @@ class Decoder:
         return torch.cat([a * c - b * s, a * s + b * c], dim=-1)
 
     def step(self) -> None:
-        """self.token in, the next token out; everything stays on the GPU."""
+        """self.token in, the next token out; everything stays on the GPU.  At most
+        max_tokens steps after a reset."""
         cfg, H, K = self.cfg, self.cfg.heads, self.cfg.kv_heads
         self.kv_len.add_(1)
         self.h.copy_(self.embedding[self.token.long()])
@@ -152,12 +153,16 @@ class Decoder:
         self.token.fill_(token)
 
     def capture(self) -> torch.cuda.CUDAGraph:
-        """The step as a graph; the state is as after reset."""
+        """The step as a graph; the state is then as after reset to the present token."""
+        token = self.token.clone()
+        self.kv_len.zero_()   # the step below must find room
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
             self.step()   # torch's own kernels are loaded outside of the capture
         torch.cuda.current_stream().wait_stream(side)
+        self.kv_len.zero_()
+        self.token.copy_(token)
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             self.step()
