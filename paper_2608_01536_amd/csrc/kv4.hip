@@ -1,10 +1,11 @@
 // The 4-bit key/value cache (include/celty_decode.h) for gfx950: writing new
 // tokens into it and reading tokens back.
 //
-// Both are bound by memory (2 x 2 D bytes of fp16 and D + 8 of cache a token
-// and head) or, for one token, by the launch; the append also by its vector
-// instructions, about 13 a channel.  3486 tokens of 32 heads x 128: append 27 us
-// (2.7 TB/s), gather 17 us (4.2 TB/s).  The unit of work is an octet:
+// The gather is bound by memory (2 x 2 D bytes of fp16 and D + 8 of cache a
+// token and head), the append by its vector instructions, 23 a channel, which
+// keep the SIMDs busy for 92 % of the time that the units are; one token is bound
+// by the launch.  3486 tokens of 32 heads x 128: append 23 us (3.1 TB/s), 18 of them
+// vector instructions, gather 16 us (4.4 TB/s).  The unit of work is an octet:
 // eight neighbouring positions of one head, which share their words of value
 // codes.  A wavefront takes an octet, lane 8 t + s holding channels
 // s D/8 .. of token t: a row's minimum and maximum are three exchanges, its

@@ -14,11 +14,15 @@
 //
 // Two kernels.  decode_kernel: 16 queries of a key head (a group's heads of one
 // token, or of a few), the positions shared out to eight wavefronts and, where
-// units are few, to several workgroups; bound by reading the cache: 5.6 TB/s at
-// 32 sequences of 16000 positions, 64 heads over 8; one sequence of 131001 takes
-// 36 us, 12 of them the launch, the first loads' round trips and the join of 32
-// workgroups.  chunk_kernel: 32 queries a wavefront; bound by vector
-// instructions (below).
+// units are few, to several workgroups; bound by reading the cache where those
+// fill the chip evenly: 64 heads over 8, 128 channels, 16 sequences of 16000
+// positions 50 us, 5.6 TB/s, 32 of them 105 us, 5.3 TB/s; one of 131001 33 us, 4.3
+// TB/s, the launch, the first loads' round trips and the join of 32 workgroups
+// among them.  Between, units are left idle: 17 sequences take 83 us (3.6 TB/s).
+// At 128 channels it takes 136 registers, three wavefronts a SIMD, so that a
+// compute unit holds one workgroup of eight; up to 128 registers it held two.
+// chunk_kernel: 32 queries a wavefront; vector and matrix instructions in turn
+// (below).
 //
 // Layout of a tile of 32 positions (16x16x32 instructions; lane = 16 g + r):
 //   scores  S^T = K Q^T, twice 16 positions: lane row r of tile h holds the
@@ -569,11 +573,13 @@ __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args 
 // one key head's group: G heads of token i, then of token i + 1) on 32x32x16
 // instructions, the four wavefronts of a workgroup neighbouring columns, all
 // walking the same positions, so that a tile comes once from L2 and is unpacked
-// for 32 columns.  Bound by vector instructions: 16 scores a lane and tile at
-// nine instructions each (one of them an exponential, two slots) and 112 for the
-// unpacking make about 1090 cycles, against 512 of the 16 matrix instructions:
-// 2048 tokens over 8192 positions, 64 heads over 8, 640 us, 750 TFLOP/s; a
-// library product of 8192^3 reaches 1130 on the same card.
+// for 32 columns.  A tile takes 269 vector instructions, 1200 cycles (16 scores a
+// lane at nine each, one of them an exponential, and 112 for the unpacking), and
+// 16 matrix instructions, 512 cycles.  By the counters the former take 75 % of
+// the SIMDs' time and the latter 32 %: a SIMD's two wavefronts overlap them
+// little, and the time is nearly their sum.  2048 tokens over 8192 positions, 64
+// heads over 8, 636 us, 755 TFLOP/s; a library product of 8192^3 reaches 1130 to
+// 1290 on the same card.
 //
 // Layout (lane = 32 h + r): score row 16 u + 8 b + 4 h + j is position
 // 8 (2 u + h) + 4 b + j, so that a lane's scores 8 u .. 8 u + 7 are the eight

@@ -7,8 +7,8 @@
 // Bound by memory where there are many rows (each operand is read once, each
 // output written once, nothing in between leaves the registers) and by the
 // launch, the loads' round trip and the reductions' barriers where there is
-// one row.  4096 x 8192 bf16, post norm and gate: 52 us, 5.2 TB/s (a copy of 1 GiB
-// reaches 5.1); 1 x 4096: 3.8 us in a graph with the post norm.  A workgroup takes
+// one row.  4096 x 8192 bf16, post norm and gate: 52 us, 5.2 TB/s (copies of its size
+// and more reach 5.2 to 5.3); 1 x 4096: 3.8 us in a graph with the post norm.  A workgroup takes
 // one row and keeps it in registers as fp32; a reduction is one wavefront tree and
 // one barrier.  Layer norms take the
 // variance about the mean, not from the sum of squares, which would cancel.
@@ -234,8 +234,8 @@ void launch_norm(NormArgs a, int rows, hipStream_t st) {
       hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(std::min<int64_t>(kGridRows, rows - a.row0))), dim3(threads), 0, st, a);
   };
   // 8 elements a thread where that fills the workgroup, 16 from 4096 on: two
-  // workgroups of 512 on a unit hide each other's reductions (4096 x 8192 56 us
-  // against 64 for one of 1024).
+  // workgroups of 512 on a unit hide each other's reductions (4096 x 8192 in a
+  // graph 49 us against 56 for one of 1024).
   auto shaped = [&](auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
     if (a.n <= 512) go(norm_kernel<T, R, 64, 1, TAIL>, 64);
