@@ -2,10 +2,10 @@
 // tokens into it and reading tokens back.
 //
 // The gather is bound by memory (2 x 2 D bytes of fp16 and D + 8 of cache a
-// token and head), the append by its vector instructions, 23 a channel, which
-// keep the SIMDs busy for 92 % of the time that the units are; one token is bound
-// by the launch.  3486 tokens of 32 heads x 128: append 23 us (3.1 TB/s), 18 of them
-// vector instructions, gather 16 us (4.4 TB/s).  The unit of work is an octet:
+// token and head), the append mostly by its vector instructions, 23 a channel;
+// one token is bound by the launch.  3486 tokens of 32 heads x 128: append 23 us
+// (3.1 TB/s), 19 of them vector instructions on all SIMDs, gather 16 us (4.4
+// TB/s).  The unit of work is an octet:
 // eight neighbouring positions of one head, which share their words of value
 // codes.  A wavefront takes an octet, lane 8 t + s holding channels
 // s D/8 .. of token t: a row's minimum and maximum are three exchanges, its
