@@ -157,7 +157,8 @@ celty_status celty_kv4_gather(const celty_kv4_cache* cache, const celty_kv4_seqs
  * over the positions j of the sequence's storage with j <= p_i and, when
  * window > 0, j > p_i - window (p_i the token's position).  A token that sees
  * no position gets zeros; one that sees any gets NaN for a query that is not
- * finite or for a NaN key or value among them.  Query head h reads key head h / (heads / kv_heads).
+ * finite or for a NaN key or value among them.  Query head h reads key head
+ * h / (heads / kv_heads).
  *   dtype      CELTY_F16 or CELTY_BF16: q and out, [n_tokens][heads][D].
  *   heads      a multiple of kv_heads.
  *   scale      finite.
@@ -217,7 +218,9 @@ typedef struct celty_filters {
  *           +infinity.  May be NULL: every row takes its largest logit.
  *   tokens  device int32[rows]; -1 for a row with no number to choose.
  * Weights are summed as multiples of 2^-38 of the largest, in 64-bit integers:
- * the result does not depend on timing.
+ * the result does not depend on timing.  A row whose cut by top_k or top_p falls
+ * among more than 4096 tokens of nearly one logit takes about 6 us per thousand
+ * logits, for one workgroup finishes it.
  *   workspace  device, at least celty_sample_workspace_bytes(rows, V) bytes (45
  *           KB a row, for 1024 rows at most), any contents; calls that may
  *           overlap need workspaces of their own.
