@@ -252,7 +252,7 @@ template <int N, typename S>
 __device__ __forceinline__ float raise_reference(float xc, float sc, float cs, S& s, float (&x)[N]) {
   const bool before = s.limit > kLow, seen = before || xc > kLow;   // nothing seen: all sums are zero, or NaN
   const float rise = before ? fmaxf(xc, 0.0f) : seen ? xc : 0.0f;
-  s.vmax = fmaxf(s.vmax, sc);
+  s.vmax = fmaxf(s.vmax, fminf(sc, 65504.0f));   // infinity shows in the product
   const float shift = kHeadroom - __builtin_amdgcn_logf(s.vmax);   // to base 2; what it rounds to is kept in s.shift
   const float r = before ? __builtin_amdgcn_exp2f(fmaf(-cs, rise, shift - s.shift)) : 1.0f;
   s.top += rise, s.shift = shift;

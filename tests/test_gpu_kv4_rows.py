@@ -203,3 +203,23 @@ def test_norm_operands_beside_each_other(env):  # noqa: F811
     one[:, 0], one[:, 1] = h, b
     celty.celty_block_norm(one[:, 0], one[:, 1], one[:, 2], one[:, 3], w_pre=w)
     assert torch.equal(one[:, 0], h) and torch.equal(one[:, 1], b) and torch.equal(one[:, 2], h_out) and torch.equal(one[:, 3], x)
+
+
+@pytest.mark.parametrize("which", list(WINDOWED))
+def test_an_infinite_value_scale_that_is_seen(env, which):  # noqa: F811
+    """What such a value stands for is not finite, and so is the result, in the
+    head that reads it; it does not look like nothing seen."""
+    torch, celty = env
+    n, m, heads, kv_heads, window, only = WINDOWED[which]
+    s = Sequences(env, [n], [m], kv_heads, 64, 32, "float16", seed=38)
+    s.fill()
+    q, out, ws = _attend(env, s, heads, window=window, only=only)
+    at = n - m - 3   # the first tokens of the call see it, the last may not
+    page, slot = int(s.table[0, at // s.page]), at % s.page
+    s.cache.v_params[page, 0, slot, 0] = float("inf")
+    got = torch.zeros_like(out)
+    celty.celty_kv4_attention(s.cache, s.seqs, q, got, ws, window=window)
+    sees = torch.arange(n - m, n, device="cuda") - window < at
+    group = heads // kv_heads
+    assert not got[sees][:, :group].isfinite().any()
+    assert torch.equal(got[~sees], out[~sees]) and torch.equal(got[:, group:], out[:, group:])
