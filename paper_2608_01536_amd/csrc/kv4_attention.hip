@@ -578,8 +578,8 @@ __global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_kernel(Kv4Args 
 // 16 matrix instructions, 512 cycles.  By the counters the former take 75 % of
 // the SIMDs' time and the latter 32 %: a SIMD's two wavefronts overlap them
 // little, and the time is nearly their sum.  2048 tokens over 8192 positions, 64
-// heads over 8, 636 us, 755 TFLOP/s; a library product of 8192^3 reaches 1130 to
-// 1290 on the same card.
+// heads over 8, 615 to 650 us by the card, 740 to 780 TFLOP/s; a library product
+// of 8192^3 reaches 1130 to 1290.
 //
 // Layout (lane = 32 h + r): score row 16 u + 8 b + 4 h + j is position
 // 8 (2 u + h) + 4 b + j, so that a lane's scores 8 u .. 8 u + 7 are the eight
