@@ -217,8 +217,9 @@ typedef struct celty_filters {
  *           token is kept, in a row without top_k, top_p and min_p everywhere.  Values below 2^-126 count as 2^-126, NaN as
  *           +infinity.  May be NULL: every row takes its largest logit.
  *   tokens  device int32[rows]; -1 for a row with no number to choose.
- * Weights are summed as multiples of 2^-38 of the largest, in 64-bit integers:
- * the result does not depend on timing.  A row whose cut by top_k or top_p falls
+ * z, w and z - log(noise) are taken in fp32; weights are summed as multiples of
+ * 2^-38 of the largest, rounded down, in 64-bit integers: the result does not
+ * depend on timing.  A row whose cut by top_k or top_p falls
  * among more than 4096 tokens of nearly one logit takes about 6 us per thousand
  * logits, for one workgroup finishes it.
  *   workspace  device, at least celty_sample_workspace_bytes(rows, V) bytes (45
